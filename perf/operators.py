@@ -158,7 +158,9 @@ def _plain_loss(s):
     lse = (top + (logits - top).exp().sum(1, keepdim=True).log()).squeeze(1)
     has = s["labels"] >= 0
     at = s["labels"].clamp(min=0).long().unsqueeze(1)
-    loss = torch.where(has, lse - logits.gather(1, at).squeeze(1), torch.zeros_like(lse))
+    none = torch.zeros_like(lse)
+    loss = torch.where(has, lse - logits.gather(1, at).squeeze(1), none)
+    lse = torch.where(has, lse, none)  # nothing of a row without a label
     return x, w, logits, lse, has, at, loss
 
 
@@ -227,7 +229,7 @@ def exact(case, seed):
             rows = torch.nonzero(y >= 0).flatten()
             of_label = torch.zeros_like(total)
             of_label[rows] = total[rows] - z[rows, y[rows]]
-            lse.append(total)
+            lse.append(torch.where(y >= 0, total, torch.zeros_like(total)))
             loss.append(of_label)
             if op == "grad":
                 c = torch.zeros_like(total)
