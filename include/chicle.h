@@ -292,6 +292,82 @@ chicle_status_t chicle_partition_noalloc(int device, void *cuda_stream, int64_t 
                                          int32_t *dev_owner, int32_t *dev_members, char *host_errbuf,
                                          size_t errbuf_len);
 
+/* ---- Operators of a softmax model with a vector per id (Sec. 2.2: training by local SGD, where a task computes the
+ * gradient of a loss over its samples; the losses above have two classes or real targets and one number per id). They
+ * need no handle. All pointers named dev_* and the data of a chicle_dense_t are device memory of `device`; the work is
+ * enqueued on cuda_stream (a stream of that device) and no call synchronises, allocates or keeps anything; `device` is
+ * made current during the call and what was current before is restored. Calls on different streams may overlap as long
+ * as each has its own workspace; all may be captured into a graph. Results do not depend on timing: equal inputs give
+ * equal bits. host_errbuf (may be NULL) receives the text of an error; on CHICLE_ERR_INVALID_ARG nothing is enqueued.
+ * dev_status (may be NULL) is one word that kernels OR bits into and never clear: CHICLE_STATUS_BAD_ID (a label or id
+ * beyond the last class or row: treated as none) and CHICLE_STATUS_TIMEOUT (a bounded wait ran out: the results are
+ * not valid). ---- */
+typedef enum { CHICLE_F32 = 0, CHICLE_BF16 = 1, CHICLE_F16 = 2 } chicle_dtype_t;
+
+#define CHICLE_STATUS_BAD_ID 4u
+#define CHICLE_STATUS_TIMEOUT 8u
+
+/* A caller-owned dense matrix on the device, row-major: element (i, j) at data[i * ld + j], ld >= cols in elements. Any
+ * alignment of the element type and any ld are taken; 16-byte aligned rows save a copy. rows may be 0, rows <=
+ * 2^31 - 4097, 1 <= cols <= 65536. */
+typedef struct {
+    chicle_dtype_t type;
+    int64_t rows, cols, ld;
+    void *data;
+} chicle_dense_t;
+
+/* Softmax cross entropy of the linear map X W^T to W->rows classes: with l_iv = x_i . w_v,
+ *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, label_i},
+ * one float per row each. A row whose label is negative has no label: its loss and lse are 0, and what it holds has no
+ * effect. X and W have one type; products are summed in fp32 (fp32 operands: to fp32 accuracy), and the logits are not kept.
+ * Values that are not finite give results that are not finite. chicle_softmax_workspace gives the bytes of workspace
+ * (256-byte aligned) for the same descriptions (host only, no device is touched). */
+chicle_status_t chicle_softmax_workspace(const chicle_dense_t *X, const chicle_dense_t *W, int gradients, size_t *host_bytes);
+chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
+                                    const int32_t *dev_labels, float *dev_loss, float *dev_lse, void *dev_workspace,
+                                    size_t workspace_bytes, uint32_t *dev_status, char *host_errbuf, size_t errbuf_len);
+
+/* The same, and the gradients of  scale * sum_i weight_i loss_i  (dev_weights: one float per row, or NULL for 1; scale
+ * finite) with respect to X and W, in their types: every element of dX and dW is written (rows of dX without a label are
+ * 0). dX and dW overlap neither X, W nor each other. The logits are held for about a gigabyte of rows at a time (8 GB at
+ * most), and where there are several such pieces, dW is summed in fp32 in the workspace. */
+chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
+                                         const int32_t *dev_labels, const float *dev_weights, float scale, float *dev_loss,
+                                         float *dev_lse, const chicle_dense_t *dX, const chicle_dense_t *dW, void *dev_workspace,
+                                         size_t workspace_bytes, uint32_t *dev_status, char *host_errbuf, size_t errbuf_len);
+
+/* out_i = scale * table_{id_i} for n = out->rows ids (int32): rows of zeros for negative ids. out has the table's type and
+ * columns and does not overlap it. */
+chicle_status_t chicle_embedding(int device, void *cuda_stream, const chicle_dense_t *table, const int32_t *dev_ids, float scale,
+                                 const chicle_dense_t *out, uint32_t *dev_status, char *host_errbuf, size_t errbuf_len);
+
+/* The gradient of chicle_embedding with respect to the table: dtable_v = scale * sum of grad_i over the i with id_i = v, in
+ * ascending i within runs whose bounds depend on the ids alone, in fp32. accumulate = 0: every row of dtable is written
+ * (zeros where no id is v). accumulate = 1: added to what dtable holds; rows without an id are not touched (a table shared
+ * with the output map: first chicle_softmax_loss_grad, then this). dtable has grad's type and columns and does not overlap it. */
+chicle_status_t chicle_embedding_grad_workspace(int64_t n, int64_t rows, int64_t cols, size_t *host_bytes);
+chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, const int32_t *dev_ids, const chicle_dense_t *grad, float scale,
+                                      int accumulate, const chicle_dense_t *dtable, void *dev_workspace, size_t workspace_bytes,
+                                      uint32_t *dev_status, char *host_errbuf, size_t errbuf_len);
+
+/* One of the tensors whose common norm is taken: n contiguous elements (n may be 0), and where the clipped ones go (in
+ * itself: in place; NULL: nowhere, the norm alone). */
+typedef struct {
+    chicle_dtype_t type;
+    int64_t n;
+    const void *in;
+    void *out;
+} chicle_tensor_t;
+
+/* *dev_norm = the 2-norm of all elements of all tensors (squares summed in fp64 in a fixed order), and
+ * out = in * min(1, max_norm / (norm + 1e-6)) for each of them. A norm that is not finite leaves the elements as they are
+ * (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors is a host array, read
+ * during the call; in and out are the same or do not overlap. Workspace: CHICLE_CLIP_WORKSPACE bytes, 256-byte aligned. */
+#define CHICLE_CLIP_WORKSPACE 16384
+chicle_status_t chicle_clip_gradients(int device, void *cuda_stream, int64_t count, const chicle_tensor_t *host_tensors, float max_norm,
+                                      float *dev_norm, void *dev_workspace, size_t workspace_bytes, char *host_errbuf,
+                                      size_t errbuf_len);
+
 /* Text of the last error on this handle (library-owned, valid until the next call on the handle). With h = NULL:
  * the text of the last failed chicle_glm_create on this thread. Never NULL. */
 const char *chicle_last_error(const chicle_glm_t *h);

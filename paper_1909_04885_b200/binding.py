@@ -27,7 +27,9 @@ EXPORTED = ["chicle_glm_create", "chicle_partition", "chicle_cocoa_round", "chic
             "chicle_last_error", "chicle_glm_destroy", "chicle_partition_noalloc", "chicle_partition_sizes",
             "chicle_cocoa_round_steps", "chicle_chunks_cut", "chicle_chunks_assign", "chicle_chunks_scale_in",
             "chicle_chunks_scale_out", "chicle_chunks_rebalance_step", "chicle_partition_chunks", "chicle_cocoa_round_delta",
-            "chicle_apply_deltas", "chicle_export_state_of", "chicle_import_state"]
+            "chicle_apply_deltas", "chicle_export_state_of", "chicle_import_state", "chicle_softmax_workspace",
+            "chicle_softmax_loss", "chicle_softmax_loss_grad", "chicle_embedding", "chicle_embedding_grad_workspace",
+            "chicle_embedding_grad", "chicle_clip_gradients"]
 
 
 class ChicleError(RuntimeError):
@@ -39,6 +41,10 @@ class ChicleError(RuntimeError):
 class Matrix(C.Structure):
     _fields_ = [("fmt", C.c_int), ("space", C.c_int), ("n_rows", C.c_int64), ("n_cols", C.c_int64), ("nnz", C.c_int64),
                 ("ld", C.c_int64), ("indptr", C.c_void_p), ("indices", C.c_void_p), ("values", C.c_void_p)]
+
+
+class Dense(C.Structure):
+    _fields_ = [("type", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("data", C.c_void_p)]
 
 
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_void_p, C.c_size_t)
@@ -119,6 +125,18 @@ def load():
     lib.chicle_glm_destroy.argtypes = [vp]
     lib.chicle_partition_noalloc.restype = C.c_int
     lib.chicle_partition_noalloc.argtypes = [C.c_int, vp, i64, i32, u64, vp, vp, C.c_char_p, C.c_size_t]
+    dp, sz = C.POINTER(Dense), C.c_size_t
+    tail = [vp, sz, vp, C.c_char_p, sz]  # workspace, its bytes, status word, error text, its bytes
+    for name, args in (("chicle_softmax_workspace", [dp, dp, C.c_int, C.POINTER(sz)]),
+                       ("chicle_softmax_loss", [C.c_int, vp, dp, dp, vp, vp, vp] + tail),
+                       ("chicle_softmax_loss_grad", [C.c_int, vp, dp, dp, vp, vp, f32, vp, vp, dp, dp] + tail),
+                       ("chicle_embedding", [C.c_int, vp, dp, vp, f32, dp, vp, C.c_char_p, sz]),
+                       ("chicle_embedding_grad_workspace", [i64, i64, i64, C.POINTER(sz)]),
+                       ("chicle_embedding_grad", [C.c_int, vp, vp, dp, f32, C.c_int, dp] + tail),
+                       ("chicle_clip_gradients", [C.c_int, vp, i64, vp, f32, vp, vp, sz, C.c_char_p, sz])):
+        fn = getattr(lib, name)
+        fn.restype = C.c_int
+        fn.argtypes = args
     _lib = lib
     return lib
 
@@ -425,3 +443,223 @@ def chunks_rebalance_step(task, chunk_off, K: int, time_per_sample):
     if r < 0:
         raise ValueError("chicle_chunks_rebalance_step: bad arguments")
     return out, bool(r)
+
+
+# ---- operators of a softmax model with a vector per id ------------------------------------------------------------
+# CUDA tensors in, CUDA tensors out; the work is enqueued on torch's current stream of the tensors' device, or on `stream`
+# (a cudaStream_t), and outputs and workspaces come from torch's caching allocator for that stream. Nothing is kept between
+# calls, no call synchronises, all can be captured into a CUDA graph. No autograd graph is recorded. `status`: an optional
+# int32 CUDA tensor of one element whose bits the kernels set (STATUS_BAD_ID: a label or id beyond the last class or row,
+# taken as none; STATUS_TIMEOUT: the results are not valid).
+STATUS_BAD_ID, STATUS_TIMEOUT = 4, 8
+CLIP_WORKSPACE = 16384
+_ERR_LEN = 256
+_dtypes = None
+
+
+def _types():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _dtypes
+
+
+def _dense(t, what: str) -> Dense:
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor of two dimensions" % what)
+    ty = _types().get(t.dtype)
+    if ty is None:
+        raise ValueError("%s must be float32, bfloat16 or float16" % what)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % what)
+    return Dense(ty, rows, cols, t.stride(0) if rows > 1 else cols, t.data_ptr())
+
+
+def _vector(t, n: int, dtype, device: int, what: str) -> int:
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on the same device" % (what, str(dtype)[6:], n))
+    return t.data_ptr()
+
+
+def _status_ptr(status, device: int):
+    if status is None:
+        return None
+    import torch
+    if status.dtype != torch.int32 or status.numel() != 1 or status.get_device() != device:
+        raise ValueError("status must be an int32 tensor of one element on the same device")
+    return status.data_ptr()
+
+
+class _On:
+    """Makes the caller's stream torch's current one while outputs and workspaces are allocated."""
+
+    def __init__(self, stream: int, device: int):
+        import torch
+        self._ctx = torch.cuda.stream(torch.cuda.ExternalStream(stream, device="cuda:%d" % device))
+
+    def __enter__(self):
+        return self._ctx.__enter__()
+
+    def __exit__(self, *exc):
+        return self._ctx.__exit__(*exc)
+
+
+def _operator(fn):
+    """Adds the keyword ``stream`` to an operator."""
+    import functools
+
+    @functools.wraps(fn)
+    def call(first, *args, stream: Optional[int] = None, **kw):
+        if stream is None:
+            return fn(first, *args, **kw)
+        t = first if hasattr(first, "get_device") else first[0]
+        with _On(stream, t.get_device()):
+            return fn(first, *args, **kw)
+    return call
+
+
+def _raw_stream(device: int) -> int:
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _workspace(nbytes: int, like):
+    return like.new_empty(nbytes, dtype=_u8()) if nbytes else None
+
+
+def _u8():
+    import torch
+    return torch.uint8
+
+
+def _raise(st: int, buf):
+    if st != OK:
+        raise ChicleError(st, buf.value.decode())
+
+
+def _softmax(x, w, labels, grad: bool, weights=None, scale=1.0, status=None):
+    import torch
+    lib = load()
+    dx, dw = _dense(x, "x"), _dense(w, "w")
+    device = x.get_device()
+    if w.get_device() != device:
+        raise ValueError("x and w must be on one device")
+    n = dx.rows
+    lp = _vector(labels, n, torch.int32, device, "labels")
+    wp = None if weights is None else _vector(weights, n, torch.float32, device, "weights")
+    sp = _status_ptr(status, device)
+    need = C.c_size_t()
+    if lib.chicle_softmax_workspace(C.byref(dx), C.byref(dw), int(grad), C.byref(need)) != OK:
+        raise ChicleError(ERR_INVALID_ARG, "x and w must have one type and the same columns, w at least one row")
+    ws = _workspace(need.value, x)
+    loss = torch.empty(n, dtype=torch.float32, device=x.device)
+    lse = torch.empty(n, dtype=torch.float32, device=x.device)
+    buf = C.create_string_buffer(_ERR_LEN)
+    stream, wsp = _raw_stream(device), None if ws is None else ws.data_ptr()
+    if not grad:
+        _raise(lib.chicle_softmax_loss(device, stream, C.byref(dx), C.byref(dw), lp, loss.data_ptr(), lse.data_ptr(), wsp,
+                                       need.value, sp, buf, _ERR_LEN), buf)
+        return loss, lse
+    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    gw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+    _raise(lib.chicle_softmax_loss_grad(device, stream, C.byref(dx), C.byref(dw), lp, wp, scale, loss.data_ptr(), lse.data_ptr(),
+                                        C.byref(_dense(gx, "dx")), C.byref(_dense(gw, "dw")), wsp, need.value, sp, buf, _ERR_LEN), buf)
+    return loss, lse, gx, gw
+
+
+@_operator
+def softmax_loss(x, w, labels, status=None):
+    """``chicle_softmax_loss``: softmax cross entropy of the linear map ``x @ w.T`` (x: n x d, w: classes x d, one type of
+    float32, bfloat16, float16) against int32 ``labels`` (negative: none). Returns (loss, lse), n float32 each; both are 0
+    for rows without a label. The logits are not kept."""
+    return _softmax(x, w, labels, False, status=status)
+
+
+@_operator
+def softmax_loss_grad(x, w, labels, weights=None, scale: float = 1.0, status=None):
+    """``chicle_softmax_loss_grad``: also the gradients of ``scale * sum(weights * loss)`` with respect to x and w, in their
+    types. Returns (loss, lse, dx, dw). ``weights``: n float32, or None for 1."""
+    return _softmax(x, w, labels, True, weights, scale, status)
+
+
+@_operator
+def embedding(table, ids, scale: float = 1.0, out=None, status=None):
+    """``chicle_embedding``: ``scale * table[ids]`` for int32 ids (one dimension), rows of zeros for negative ids."""
+    import torch
+    lib = load()
+    dt = _dense(table, "table")
+    device = table.get_device()
+    n = ids.shape[0]
+    ip = _vector(ids, n, torch.int32, device, "ids")
+    if out is None:
+        out = torch.empty((n, dt.cols), dtype=table.dtype, device=table.device)
+    elif out.get_device() != device or out.shape[0] != n:
+        raise ValueError("out must have a row per id and be on the table's device")
+    do = _dense(out, "out")
+    buf = C.create_string_buffer(_ERR_LEN)
+    _raise(lib.chicle_embedding(device, _raw_stream(device), C.byref(dt), ip, scale, C.byref(do), _status_ptr(status, device), buf, _ERR_LEN), buf)
+    return out
+
+
+@_operator
+def embedding_grad(ids, grad, rows: int, scale: float = 1.0, out=None, accumulate: bool = False, status=None):
+    """``chicle_embedding_grad``: ``scale *`` the sum of the rows of ``grad`` (n x d) by id, as a table of ``rows`` rows;
+    negative ids are left out. ``accumulate``: added to ``out``, whose other rows are left as they are."""
+    import torch
+    lib = load()
+    dg = _dense(grad, "grad")
+    device = grad.get_device()
+    ip = _vector(ids, dg.rows, torch.int32, device, "ids")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((rows, dg.cols), dtype=grad.dtype, device=grad.device)
+    elif out.get_device() != device or out.shape[0] != rows:
+        raise ValueError("out must have `rows` rows and be on the gradient's device")
+    dt = _dense(out, "out")
+    need = C.c_size_t()
+    if lib.chicle_embedding_grad_workspace(dg.rows, rows, dg.cols, C.byref(need)) != OK:
+        raise ChicleError(ERR_INVALID_ARG, "sizes out of range")
+    ws = _workspace(need.value, grad)
+    buf = C.create_string_buffer(_ERR_LEN)
+    _raise(lib.chicle_embedding_grad(device, _raw_stream(device), ip, C.byref(dg), scale, int(bool(accumulate)), C.byref(dt),
+                                     None if ws is None else ws.data_ptr(), need.value, _status_ptr(status, device), buf, _ERR_LEN), buf)
+    return out
+
+
+@_operator
+def clip_gradients(tensors, max_norm: float, out=None):
+    """``chicle_clip_gradients``: returns the 2-norm of all elements of all ``tensors`` (a float32 tensor without dimensions)
+    and multiplies them by ``min(1, max_norm / (norm + 1e-6))``, in place or into the tensors of ``out`` (as many, of the same
+    types and lengths). A norm that is not finite leaves the elements as they are. ``max_norm=inf``: the norm alone."""
+    import array
+    import torch
+    lib = load()
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("no tensors")
+    types = _types()
+    device = tensors[0].get_device()
+    kinds = [types.get(t.dtype, -1) for t in tensors]
+    lens = [t.numel() for t in tensors]
+    ins = [t.data_ptr() for t in tensors]
+    # (a tensor on the host has device -1)
+    good = device >= 0 and -1 not in kinds and all([t.is_contiguous() and t.get_device() == device for t in tensors])
+    outs = ins
+    if out is not None:
+        out = list(out)
+        good = good and len(out) == len(tensors) and lens == [t.numel() for t in out] and kinds == [types.get(t.dtype, -1) for t in out]
+        good = good and all([t.is_contiguous() and t.get_device() == device for t in out])
+        outs = [t.data_ptr() for t in out]
+    if not good:
+        raise ValueError("the tensors must be contiguous CUDA tensors of float32, bfloat16 or float16 on one device, and those of "
+                         "out of the same number, types and lengths")
+    table = array.array("q", [v for four in zip(kinds, lens, ins, outs) for v in four])  # chicle_tensor_t: four words
+    ws = tensors[0].new_empty(CLIP_WORKSPACE, dtype=torch.uint8)
+    norm = torch.empty((), dtype=torch.float32, device=tensors[0].device)
+    buf = C.create_string_buffer(_ERR_LEN)
+    _raise(lib.chicle_clip_gradients(device, _raw_stream(device), len(tensors), table.buffer_info()[0], max_norm, norm.data_ptr(),
+                                     ws.data_ptr(), CLIP_WORKSPACE, buf, _ERR_LEN), buf)
+    return norm

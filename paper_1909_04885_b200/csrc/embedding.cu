@@ -1,0 +1,628 @@
+// Embedding lookup with scaling, and its gradient by sorted ids (chicle_embedding, chicle_embedding_grad): the product of
+// a row of ids with a model that has a vector per id, and the sum of the rows' gradients per id.
+//
+//   out_i = s T[id_i]                dT_v = s sum_{i: id_i = v} G_i
+//
+// Both are bound by memory. The gradient sorts (id, position) pairs, stably, so that the terms of an id are added in one
+// order whatever the timing: up to 4096 ids each position counts the ones in front of it (n^2 comparisons, one launch),
+// above that by radix passes of up to 10 bits. The sorted entries are cut into windows of equal length; a window sums
+// its runs of equal ids, writes those that lie inside it and leaves the ones that cross its ends as partial sums in fp32, which
+// a last kernel adds in order. So an id with most of the entries takes no longer than many ids with a few.
+// Rows without an id are zeroed by further CTAs of the same kernels.
+#include <algorithm>
+#include <cmath>
+
+#include "operators.cuh"
+
+namespace chicle {
+namespace {
+
+constexpr int kMaxRankN = 4096;   // ids sorted by counting
+constexpr int kTile = 4096;       // entries per CTA of a radix pass
+constexpr int kTileThreads = 512;
+constexpr int kDigits = 1024;
+constexpr int kGroupTiles = 32;   // tiles whose digit counts are added up in advance
+constexpr int64_t kTargetThreads = 148 * 1024;
+constexpr int64_t kZeroBytes = 128 * 1024; // of dtable per zeroing CTA
+
+template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
+template <typename T> __device__ __forceinline__ T of_float(float v);
+template <> __device__ __forceinline__ float of_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 of_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half of_float<__half>(float v) { return __float2half_rn(v); }
+
+template <typename T, int E> struct alignas(sizeof(T) * E > 16 ? 16 : sizeof(T) * E) Vec {
+    T v[E];
+};
+
+// ---- lookup ------------------------------------------------------------------------------------------------
+
+// A thread takes one vector of R rows: R independent row reads are in flight.
+template <typename T, int E, int R>
+__global__ void __launch_bounds__(256)
+k_lookup(const T *__restrict__ table, int64_t ld, int32_t rows, const int32_t *__restrict__ ids, int64_t n, int32_t vecs, int tpr_log,
+         float scale, T *__restrict__ out, int64_t ld_out, uint32_t *status)
+{
+    const int tpr = 1 << tpr_log;
+    const int c = blockIdx.y * tpr + (threadIdx.x & (tpr - 1));
+    const int64_t i0 = ((int64_t)blockIdx.x * (256 >> tpr_log) + (threadIdx.x >> tpr_log)) * R;
+    if (c >= vecs) return;
+    Vec<T, E> q[R];
+    bool has[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int32_t id = i0 + r < n ? ids[i0 + r] : -1;
+        has[r] = (uint32_t)id < (uint32_t)rows;
+        if (id >= rows && c == 0 && status) atomicOr(status, (uint32_t)ST_BAD_INDEX);
+        if (has[r]) q[r] = *reinterpret_cast<const Vec<T, E> *>(table + (int64_t)id * ld + (int64_t)c * E);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (i0 + r >= n) break;
+        Vec<T, E> o;
+#pragma unroll
+        for (int j = 0; j < E; ++j) o.v[j] = has[r] ? of_float<T>(to_float(q[r].v[j]) * scale) : of_float<T>(0.f);
+        *reinterpret_cast<Vec<T, E> *>(out + (i0 + r) * ld_out + (int64_t)c * E) = o;
+    }
+}
+
+// ---- sorting ids -------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ int32_t key_of(int32_t id, int32_t rows, uint32_t *status)
+{
+    if (id >= rows && status) atomicOr(status, (uint32_t)ST_BAD_INDEX);
+    return (uint32_t)id < (uint32_t)rows ? id : rows; // no id: behind all others
+}
+
+// Place of every id in the sorted order: the number of smaller ones, and of equal ones in front of it. 32 ids per CTA,
+// eight threads each count an eighth.
+__global__ void __launch_bounds__(256) k_rank_ids(const int32_t *__restrict__ ids, int32_t n, int32_t rows, int32_t *__restrict__ keys,
+                                                  int32_t *__restrict__ order, uint32_t *status)
+{
+    __shared__ __align__(16) int32_t s_key[kMaxRankN];
+    __shared__ int s_part[8][32];
+    const int padded = (n + 31) & ~31;
+    for (int j = threadIdx.x; j < padded; j += 256) s_key[j] = j < n ? key_of(ids[j], rows, blockIdx.x == 0 ? status : nullptr) : INT32_MAX;
+    __syncthreads();
+    const int i = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const int32_t mine = i < n ? s_key[i] : -1;
+    const int quads = padded / 4;
+    const int q0 = quads * part / 8, q1 = quads * (part + 1) / 8;
+    int count = 0;
+    for (int q = q0; q < q1; ++q) {
+        const int4 k = reinterpret_cast<const int4 *>(s_key)[q];
+        // in front of i: equal ones count too
+        count += (k.x < mine + (4 * q < i)) + (k.y < mine + (4 * q + 1 < i)) + (k.z < mine + (4 * q + 2 < i)) + (k.w < mine + (4 * q + 3 < i));
+    }
+    s_part[part][threadIdx.x & 31] = count;
+    __syncthreads();
+    if (part == 0 && i < n) {
+        int at = 0;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) at += s_part[p][threadIdx.x];
+        keys[at] = mine;
+        order[at] = i;
+    }
+}
+
+// Digit counts of a tile: its own row of `hist`, and added to its group's row and to the total.
+__global__ void __launch_bounds__(kTileThreads) k_id_hist(const int32_t *__restrict__ in, int64_t n, int32_t rows, bool raw, int shift, int digits,
+                                                          uint32_t *__restrict__ hist, uint32_t *__restrict__ group,
+                                                          uint32_t *__restrict__ total, uint32_t *status)
+{
+    __shared__ uint32_t h[kDigits];
+    for (int j = threadIdx.x; j < digits; j += kTileThreads) h[j] = 0;
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * kTile;
+#pragma unroll
+    for (int it = 0; it < kTile / kTileThreads; ++it) {
+        const int64_t i = base + it * kTileThreads + threadIdx.x;
+        const bool live = i < n;
+        const int32_t k = live ? (raw ? key_of(in[i], rows, status) : in[i]) : 0;
+        const int dg = live ? (k >> shift) & (digits - 1) : -1;
+        // one atomic per digit of a warp: a frequent id would queue up
+        const uint32_t peers = __match_any_sync(0xffffffffu, dg);
+        if (live && (threadIdx.x & 31) == __ffs(peers) - 1) atomicAdd(&h[dg], (uint32_t)__popc(peers));
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < digits; j += kTileThreads) {
+        const uint32_t c = h[j];
+        hist[(int64_t)blockIdx.x * digits + j] = c;
+        if (c) {
+            atomicAdd(&group[(int64_t)(blockIdx.x / kGroupTiles) * digits + j], c);
+            atomicAdd(&total[j], c);
+        }
+    }
+}
+
+// Stable scatter of a tile by one digit.
+__global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__restrict__ in, const int32_t *__restrict__ order_in, int64_t n,
+                                                             int32_t rows, bool raw, int shift, int digits, const uint32_t *__restrict__ hist,
+                                                             const uint32_t *__restrict__ group, const uint32_t *__restrict__ total,
+                                                             int32_t *__restrict__ keys, int32_t *__restrict__ order)
+{
+    constexpr int kWarps = kTileThreads / 32, kItems = kTile / kTileThreads;
+    extern __shared__ uint32_t smem[];
+    uint32_t(*cnt)[kDigits] = reinterpret_cast<uint32_t(*)[kDigits]>(smem); // [warp][digit]
+    __shared__ uint32_t s_scan[kWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int j = threadIdx.x; j < kWarps * kDigits; j += kTileThreads) smem[j] = 0;
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * kTile + (int64_t)warp * (kItems * 32);
+    const uint32_t below = (1u << lane) - 1u;
+    int32_t key[kItems], dig[kItems];
+    uint32_t rank[kItems];
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+        const int64_t i = base + it * 32 + lane;
+        key[it] = i < n ? (raw ? key_of(in[i], rows, nullptr) : in[i]) : 0;
+        dig[it] = i < n ? (key[it] >> shift) & (digits - 1) : -1;
+    }
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+        const int d = dig[it];
+        const uint32_t peers = __match_any_sync(0xffffffffu, d);
+        const uint32_t before = d >= 0 ? cnt[warp][d] : 0u;
+        __syncwarp();
+        if (d >= 0 && (peers & below) == 0u) cnt[warp][d] = before + __popc(peers);
+        __syncwarp();
+        rank[it] = before + __popc(peers & below);
+    }
+    // where a digit's entries of this tile begin: digits in front (scan of the totals), groups and tiles in front
+    const int g = blockIdx.x / kGroupTiles;
+    uint32_t tot[2], own[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int d = threadIdx.x * 2 + k;
+        tot[k] = own[k] = 0;
+        if (d < digits) {
+            tot[k] = total[d];
+            for (int j = 0; j < g; ++j) own[k] += group[(int64_t)j * digits + d];
+            for (int j = g * kGroupTiles; j < (int)blockIdx.x; ++j) own[k] += hist[(int64_t)j * digits + d];
+        }
+    }
+    uint32_t inc = tot[0] + tot[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) s_scan[warp] = inc;
+    __syncthreads(); // (the warps' counters are complete, too)
+    uint32_t start = inc - tot[0] - tot[1];
+    for (int w = 0; w < warp; ++w) start += s_scan[w];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int d = threadIdx.x * 2 + k;
+        if (d < digits) {
+            uint32_t run = start + own[k];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const uint32_t c = cnt[w][d];
+                cnt[w][d] = run;
+                run += c;
+            }
+        }
+        start += tot[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+        const int64_t i = base + it * 32 + lane;
+        if (i < n) {
+            const uint32_t at = cnt[warp][dig[it]] + rank[it];
+            keys[at] = key[it];
+            order[at] = raw ? (int32_t)i : order_in[i];
+        }
+    }
+}
+
+// ---- sums by id --------------------------------------------------------------------------------------------
+
+// First entry of keys[0, n) that is >= v; a whole warp.
+__device__ __forceinline__ int32_t first_not_below(const int32_t *__restrict__ keys, int32_t n, int32_t v)
+{
+    const int lane = threadIdx.x & 31;
+    int32_t lo = 0, len = n; // the answer lies in [lo, lo + len]
+    while (len > 0) {
+        const int32_t step = (len + 31) / 32;
+        const int32_t at = lo + lane * step;
+        const uint32_t below = __ballot_sync(0xffffffffu, at < lo + len && keys[at] < v);
+        const int32_t k = __popc(below); // the first k probes are below v
+        if (k == 0) break;
+        const int32_t end = lo + len;
+        lo += (k - 1) * step + 1;
+        len = min(step - 1, end - lo);
+    }
+    return lo;
+}
+
+struct Sums {
+    const int32_t *keys, *order;
+    int64_t n;
+    int32_t rows, d, vecs;
+    int tpr_log, slabs;   // threads per row and slabs of a row
+    int64_t window, windows;
+    float scale;
+    int accumulate;
+    float *partial;       // [window][2][d]: of the run that came in, of the run that goes out
+    int64_t sum_blocks, zero_rows; // CTAs that sum, rows per zeroing CTA
+};
+
+template <typename T, int E>
+__device__ __forceinline__ void put_row(const Sums &s, T *table, int64_t ld, int32_t v, int c, const float (&acc)[E])
+{
+    T *at = table + (int64_t)v * ld + (int64_t)c * E;
+    Vec<T, E> o;
+    if (s.accumulate) {
+        o = *reinterpret_cast<const Vec<T, E> *>(at);
+#pragma unroll
+        for (int j = 0; j < E; ++j) o.v[j] = of_float<T>(to_float(o.v[j]) + acc[j] * s.scale);
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) o.v[j] = of_float<T>(acc[j] * s.scale);
+    }
+    *reinterpret_cast<Vec<T, E> *>(at) = o;
+}
+
+template <int E> __device__ __forceinline__ void put_partial(const Sums &s, int64_t at, int c, const float (&acc)[E])
+{
+    Vec<float, E> o;
+#pragma unroll
+    for (int j = 0; j < E; ++j) o.v[j] = acc[j];
+    *reinterpret_cast<Vec<float, E> *>(s.partial + at * s.d + (int64_t)c * E) = o;
+}
+
+template <typename T, int E>
+__global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__restrict__ grad, int64_t ld, T *__restrict__ table, int64_t ld_t)
+{
+    if (blockIdx.x >= s.sum_blocks) {
+        // rows without an id
+        __shared__ uint32_t s_has[32];
+        const int64_t v0 = (int64_t)(blockIdx.x - s.sum_blocks) * s.zero_rows, v1 = min(v0 + s.zero_rows, (int64_t)s.rows);
+        __shared__ int32_t s_first;
+        if (threadIdx.x < 32) {
+            s_has[threadIdx.x] = 0;
+            const int32_t f = first_not_below(s.keys, (int32_t)s.n, (int32_t)v0);
+            if (threadIdx.x == 0) s_first = f;
+        }
+        __syncthreads();
+        for (int64_t e = s_first + (int64_t)threadIdx.x; e < s.n; e += 256) {
+            const int32_t k = s.keys[e];
+            if (k >= v1) break;
+            const int b = (int)(k - v0);
+            if (e == 0 || s.keys[e - 1] != k) atomicOr(&s_has[b >> 5], 1u << (b & 31));
+        }
+        __syncthreads();
+        Vec<T, E> none;
+#pragma unroll
+        for (int j = 0; j < E; ++j) none.v[j] = of_float<T>(0.f);
+        for (int64_t v = v0 + (threadIdx.x >> s.tpr_log); v < v1; v += 256 >> s.tpr_log) {
+            const int b = (int)(v - v0);
+            if ((s_has[b >> 5] >> (b & 31)) & 1u) continue;
+            Vec<T, E> *row = reinterpret_cast<Vec<T, E> *>(table + v * ld_t);
+            for (int c = threadIdx.x & ((1 << s.tpr_log) - 1); c < s.vecs; c += 1 << s.tpr_log) row[c] = none;
+        }
+        return;
+    }
+    const int tpr = 1 << s.tpr_log, per = 256 >> s.tpr_log;
+    const int64_t slab = blockIdx.x % s.slabs, wb = blockIdx.x / s.slabs;
+    const int c = (int)slab * tpr + (threadIdx.x & (tpr - 1));
+    const int64_t w = wb * per + (threadIdx.x >> s.tpr_log);
+    if (c >= s.vecs || w >= s.windows) return;
+    const int64_t e0 = w * s.window, e1 = min(e0 + s.window, s.n);
+    float acc[E];
+    int32_t cur = s.keys[e0];
+    bool from_before = e0 > 0 && s.keys[e0 - 1] == cur;
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] = 0.f;
+    constexpr int kAhead = 8;
+    for (int64_t e = e0; e < e1; e += kAhead) {
+        int32_t key[kAhead];
+        Vec<T, E> q[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            key[a] = e + a < e1 ? s.keys[e + a] : s.rows;
+            if (key[a] < s.rows) q[a] = *reinterpret_cast<const Vec<T, E> *>(grad + (int64_t)s.order[e + a] * ld + (int64_t)c * E);
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (e + a >= e1) break;
+            if (key[a] != cur) {
+                if (from_before) {
+                    put_partial<E>(s, w * 2, c, acc);
+                    from_before = false;
+                } else {
+                    put_row<T, E>(s, table, ld_t, cur, c, acc);
+                }
+#pragma unroll
+                for (int j = 0; j < E; ++j) acc[j] = 0.f;
+                cur = key[a];
+            }
+            if (cur >= s.rows) return; // from here on entries without an id
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] += to_float(q[a].v[j]);
+        }
+    }
+    const bool goes_on = e1 < s.n && s.keys[e1] == cur;
+    if (!from_before && !goes_on) {
+        put_row<T, E>(s, table, ld_t, cur, c, acc);
+    } else {
+        put_partial<E>(s, w * 2 + (from_before ? 0 : 1), c, acc);
+    }
+}
+
+// Adds the partial sums of runs that cross windows: the CTA of the window where a run begins. Its groups of threads
+// take consecutive windows each, and their sums are added in order.
+template <typename T, int E>
+__global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restrict__ table, int64_t ld_t)
+{
+    __shared__ float s_sum[256][E];
+    const int64_t w = blockIdx.x;
+    const int64_t e0 = w * s.window, e1 = min(e0 + s.window, s.n);
+    if (e1 >= s.n) return;
+    const int32_t k = s.keys[e1];
+    if (s.keys[e1 - 1] != k || k >= s.rows) return;
+    if (s.keys[e0] == k && e0 > 0 && s.keys[e0 - 1] == k) return; // begins in an earlier window
+    const int64_t end = first_not_below(s.keys + e1, (int32_t)(s.n - e1), k + 1) + e1;
+    const int64_t last = (end - 1) / s.window; // windows w + 1 .. last hold the rest
+    const int tpr = 1 << s.tpr_log, groups = 256 >> s.tpr_log;
+    const int c = blockIdx.y * tpr + (threadIdx.x & (tpr - 1)), g = threadIdx.x >> s.tpr_log;
+    const int64_t count = last - w + 1;
+    float acc[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] = 0.f;
+    if (c < s.vecs) {
+        const int64_t a = count * g / groups, b = count * (g + 1) / groups;
+#pragma unroll 8
+        for (int64_t i = a; i < b; ++i) {
+            const Vec<float, E> p = *reinterpret_cast<const Vec<float, E> *>(s.partial + ((w + i) * 2 + (i == 0 ? 1 : 0)) * s.d + (int64_t)c * E);
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] += p.v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) s_sum[threadIdx.x][j] = acc[j];
+    __syncthreads();
+    if (g == 0 && c < s.vecs) {
+        for (int o = 1; o < groups; ++o)
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] += s_sum[threadIdx.x + (o << s.tpr_log)][j];
+        put_row<T, E>(s, table, ld_t, k, c, acc);
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------
+
+int log2_up(int64_t v)
+{
+    int l = 0;
+    while (((int64_t)1 << l) < v) ++l;
+    return l;
+}
+
+struct IdPlan {
+    int passes = 0, digit_bits = 0;
+    int64_t tiles = 0, groups = 0;
+    int64_t window = 0, windows = 0;
+    size_t keys[2], order[2], hist, group, total, partial, bytes; // offsets; group and total of all passes lie together
+    size_t zero_at, zero_bytes;
+};
+
+// Windows: long enough that about kTargetThreads threads share the work, eight entries at least.
+IdPlan make_plan(int64_t n, int64_t rows, int64_t cols)
+{
+    IdPlan p;
+    size_t at = 0;
+    auto take = [&](size_t b) {
+        const size_t here = at;
+        at += (b + 255) / 256 * 256;
+        return here;
+    };
+    const int64_t threads_per_row = std::max<int64_t>(1, cols / 8);
+    const int64_t want = std::max<int64_t>(1, kTargetThreads / threads_per_row);
+    p.window = 8;
+    while (p.window < 4096 && ceil_div(n, p.window) > want) p.window *= 2;
+    p.windows = ceil_div(n, p.window);
+    for (int k = 0; k < 2; ++k) {
+        p.keys[k] = take((size_t)n * 4);
+        p.order[k] = take((size_t)n * 4);
+    }
+    if (n > kMaxRankN) {
+        const int bits = log2_up(rows + 1);
+        p.passes = (int)std::max<int64_t>(1, ceil_div(bits, 10));
+        p.digit_bits = (int)ceil_div(bits, p.passes);
+        p.tiles = ceil_div(n, kTile);
+        p.groups = ceil_div(p.tiles, kGroupTiles);
+        const size_t digits = (size_t)1 << p.digit_bits;
+        p.hist = take((size_t)p.tiles * digits * 4);
+        p.zero_at = at;
+        p.group = take((size_t)p.passes * p.groups * digits * 4);
+        p.total = take((size_t)p.passes * digits * 4);
+        p.zero_bytes = at - p.zero_at;
+    }
+    p.partial = take((size_t)p.windows * 2 * cols * 4);
+    p.bytes = at;
+    return p;
+}
+
+// Sorted keys and order are in buffer `which` afterwards.
+cudaError_t sort_ids(const IdPlan &p, const int32_t *ids, int64_t n, int32_t rows, uint8_t *ws, uint32_t *status, cudaStream_t s, int *which)
+{
+    int32_t *keys[2] = {reinterpret_cast<int32_t *>(ws + p.keys[0]), reinterpret_cast<int32_t *>(ws + p.keys[1])};
+    int32_t *order[2] = {reinterpret_cast<int32_t *>(ws + p.order[0]), reinterpret_cast<int32_t *>(ws + p.order[1])};
+    *which = 0;
+    if (n <= kMaxRankN) {
+        k_rank_ids<<<(unsigned)ceil_div(n, 32), 256, 0, s>>>(ids, (int32_t)n, rows, keys[0], order[0], status);
+        return cudaGetLastError();
+    }
+    constexpr int kSmem = kTileThreads / 32 * kDigits * 4;
+    cudaError_t e = cudaFuncSetAttribute(k_id_scatter, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e == cudaSuccess) e = cudaMemsetAsync(ws + p.zero_at, 0, p.zero_bytes, s);
+    const int digits = 1 << p.digit_bits;
+    for (int k = 0; e == cudaSuccess && k < p.passes; ++k) {
+        const bool raw = k == 0;
+        const int32_t *in = raw ? ids : keys[(k + 1) & 1];
+        uint32_t *hist = reinterpret_cast<uint32_t *>(ws + p.hist);
+        uint32_t *group = reinterpret_cast<uint32_t *>(ws + p.group) + (size_t)k * p.groups * digits;
+        uint32_t *total = reinterpret_cast<uint32_t *>(ws + p.total) + (size_t)k * digits;
+        k_id_hist<<<(unsigned)p.tiles, kTileThreads, 0, s>>>(in, n, rows, raw, k * p.digit_bits, digits, hist, group, total, status);
+        k_id_scatter<<<(unsigned)p.tiles, kTileThreads, kSmem, s>>>(in, order[(k + 1) & 1], n, rows, raw, k * p.digit_bits, digits, hist, group,
+                                                                    total, keys[k & 1], order[k & 1]);
+        e = cudaGetLastError();
+        *which = k & 1;
+    }
+    return e;
+}
+
+int size_of(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
+
+// Elements per access: the largest power of two up to 16 bytes that divides addresses, row pitches and the row length.
+int vector_elements(const chicle_dense_t &a, const chicle_dense_t &b)
+{
+    const int es = size_of(a.type);
+    uint64_t bits = 16u | reinterpret_cast<uintptr_t>(a.data) | reinterpret_cast<uintptr_t>(b.data) | (uint64_t)a.cols * es;
+    if (a.rows > 1) bits |= (uint64_t)a.ld * es;
+    if (b.rows > 1) bits |= (uint64_t)b.ld * es;
+    const uint64_t low = bits & (~bits + 1);
+    return (int)std::max<uint64_t>(1, low / es);
+}
+
+template <typename T, int E>
+cudaError_t lookup(const chicle_dense_t &t, const int32_t *ids, float scale, const chicle_dense_t &o, uint32_t *status, cudaStream_t s)
+{
+    const int vecs = (int)(t.cols / E);
+    const int tpr_log = std::min(8, log2_up(vecs));
+    const unsigned slabs = (unsigned)ceil_div(vecs, 1 << tpr_log);
+    const int64_t per = 256 >> tpr_log;
+    // four rows per thread where that leaves every SM its CTAs
+    if (ceil_div(o.rows, per * 4) * slabs >= kSms * 8)
+        k_lookup<T, E, 4><<<dim3((unsigned)ceil_div(o.rows, per * 4), slabs), 256, 0, s>>>(
+            (const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
+    else
+        k_lookup<T, E, 1><<<dim3((unsigned)ceil_div(o.rows, per), slabs), 256, 0, s>>>(
+            (const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
+    return cudaGetLastError();
+}
+
+template <typename T, int E>
+cudaError_t sum_by_id(Sums sm, const chicle_dense_t &g, const chicle_dense_t &t, cudaStream_t s)
+{
+    sm.vecs = (int)(g.cols / E);
+    sm.tpr_log = std::min(8, log2_up(sm.vecs));
+    sm.slabs = (int)ceil_div(sm.vecs, 1 << sm.tpr_log);
+    sm.sum_blocks = ceil_div(sm.windows, 256 >> sm.tpr_log) * sm.slabs;
+    sm.zero_rows = std::max<int64_t>(1, std::min<int64_t>(1024, kZeroBytes / (g.cols * size_of(g.type))));
+    const int64_t zero_blocks = sm.accumulate ? 0 : ceil_div(sm.rows, sm.zero_rows);
+    k_sum_by_id<T, E><<<(unsigned)(sm.sum_blocks + zero_blocks), 256, 0, s>>>(sm, (const T *)g.data, g.ld, (T *)t.data, t.ld);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && sm.windows > 1) {
+        k_join_windows<T, E><<<dim3((unsigned)sm.windows, (unsigned)sm.slabs), 256, 0, s>>>(sm, (T *)t.data, t.ld);
+        e = cudaGetLastError();
+    }
+    return e;
+}
+
+// Calls f(type's tag, elements per access) for the access width.
+template <typename T, typename F> cudaError_t by_width(int e, F f)
+{
+    constexpr int kMost = 16 / (int)sizeof(T);
+    if constexpr (kMost == 8)
+        if (e >= 8) return f(T{}, std::integral_constant<int, 8>{});
+    if (e >= 4) return f(T{}, std::integral_constant<int, 4>{});
+    if (e >= 2) return f(T{}, std::integral_constant<int, 2>{});
+    return f(T{}, std::integral_constant<int, 1>{});
+}
+template <typename F> cudaError_t by_type(chicle_dtype_t t, int e, F f)
+{
+    if (t == CHICLE_F32) return by_width<float>(e, f);
+    if (t == CHICLE_BF16) return by_width<__nv_bfloat16>(e, f);
+    return by_width<__half>(e, f);
+}
+
+bool overlapping(const chicle_dense_t &a, const chicle_dense_t &b)
+{
+    if (a.rows == 0 || b.rows == 0) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
+    const uintptr_t an = (uintptr_t)((a.rows - 1) * a.ld + a.cols) * size_of(a.type), bn = (uintptr_t)((b.rows - 1) * b.ld + b.cols) * size_of(b.type);
+    return a0 < b0 + bn && b0 < a0 + an;
+}
+
+const char *check_pair(const chicle_dense_t *a, const chicle_dense_t *b, float scale)
+{
+    if (const char *m = check_dense(a)) return m;
+    if (const char *m = check_dense(b)) return m;
+    if (a->type != b->type) return "both matrices must have one element type";
+    if (a->cols != b->cols) return "both matrices must have the same number of columns";
+    if (overlapping(*a, *b)) return "the matrices must not overlap";
+    if (!std::isfinite(scale)) return "scale must be finite";
+    return nullptr;
+}
+
+} // namespace
+} // namespace chicle
+
+using namespace chicle;
+
+extern "C" chicle_status_t chicle_embedding(int device, void *cuda_stream, const chicle_dense_t *table, const int32_t *dev_ids, float scale,
+                                            const chicle_dense_t *out, uint32_t *dev_status, char *host_errbuf, size_t errbuf_len)
+{
+    const CallError err{host_errbuf, errbuf_len};
+    if (const char *m = check_pair(table, out, scale)) return err(CHICLE_ERR_INVALID_ARG, m);
+    if (out->rows == 0) return CHICLE_OK;
+    if (!dev_ids) return err(CHICLE_ERR_INVALID_ARG, "ids must be a non-NULL device pointer");
+    const DeviceGuard guard(device);
+    if (!guard.ok()) return err(CHICLE_ERR_CUDA, guard.message());
+    const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = by_type(table->type, vector_elements(*table, *out), [&](auto tag, auto width) {
+        return lookup<decltype(tag), decltype(width)::value>(*table, dev_ids, scale, *out, dev_status, s);
+    });
+    return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
+}
+
+extern "C" chicle_status_t chicle_embedding_grad_workspace(int64_t n, int64_t rows, int64_t cols, size_t *host_bytes)
+{
+    if (!host_bytes || n < 0 || rows < 0 || cols < 1 || n > INT32_MAX - 4096 || rows > INT32_MAX - 4096 || cols > 65536)
+        return CHICLE_ERR_INVALID_ARG;
+    *host_bytes = n ? make_plan(n, rows, cols).bytes : 0;
+    return CHICLE_OK;
+}
+
+extern "C" chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, const int32_t *dev_ids, const chicle_dense_t *grad, float scale,
+                                                 int accumulate, const chicle_dense_t *dtable, void *dev_workspace, size_t workspace_bytes,
+                                                 uint32_t *dev_status, char *host_errbuf, size_t errbuf_len)
+{
+    const CallError err{host_errbuf, errbuf_len};
+    if (const char *m = check_pair(grad, dtable, scale)) return err(CHICLE_ERR_INVALID_ARG, m);
+    const int64_t n = grad->rows;
+    if (n > 0 && !dev_ids) return err(CHICLE_ERR_INVALID_ARG, "ids must be a non-NULL device pointer");
+    const IdPlan p = n ? make_plan(n, dtable->rows, grad->cols) : IdPlan{};
+    if (n > 0)
+        if (const char *m = check_workspace(dev_workspace, workspace_bytes, p.bytes)) return err(CHICLE_ERR_INVALID_ARG, m);
+    const DeviceGuard guard(device);
+    if (!guard.ok()) return err(CHICLE_ERR_CUDA, guard.message());
+    const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = cudaSuccess;
+    if (n == 0) {
+        const size_t es = (size_t)size_of(dtable->type);
+        if (!accumulate && dtable->rows > 0)
+            e = cudaMemset2DAsync(dtable->data, (size_t)dtable->ld * es, 0, (size_t)dtable->cols * es, (size_t)dtable->rows, s);
+        return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
+    }
+    uint8_t *ws = static_cast<uint8_t *>(dev_workspace);
+    int which = 0;
+    e = sort_ids(p, dev_ids, n, (int32_t)dtable->rows, ws, dev_status, s, &which);
+    if (e == cudaSuccess) {
+        Sums sm{};
+        sm.keys = reinterpret_cast<int32_t *>(ws + p.keys[which]);
+        sm.order = reinterpret_cast<int32_t *>(ws + p.order[which]);
+        sm.n = n, sm.rows = (int32_t)dtable->rows, sm.d = (int32_t)grad->cols;
+        sm.window = p.window, sm.windows = p.windows;
+        sm.scale = scale, sm.accumulate = accumulate;
+        sm.partial = reinterpret_cast<float *>(ws + p.partial);
+        e = by_type(grad->type, vector_elements(*grad, *dtable), [&](auto tag, auto width) {
+            return sum_by_id<decltype(tag), decltype(width)::value>(sm, *grad, *dtable, s);
+        });
+    }
+    return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
+}
