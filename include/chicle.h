@@ -329,7 +329,7 @@ chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_
 
 /* The same, and the gradients of  scale * sum_i weight_i loss_i  (dev_weights: one float per row, or NULL for 1; scale
  * finite) with respect to X and W, in their types: every element of dX and dW is written (rows of dX without a label are
- * 0). dX and dW overlap neither X, W nor each other. The logits are held for about a gigabyte of rows at a time (8 GB at
+ * 0). dX and dW overlap neither X, W nor each other. The logits are held for about two gigabytes of rows at a time (8 GB at
  * most), and where there are several such pieces, dW is summed in fp32 in the workspace. */
 chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
                                          const int32_t *dev_labels, const float *dev_weights, float scale, float *dev_loss,

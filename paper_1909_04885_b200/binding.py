@@ -6,8 +6,12 @@ shared library is missing, loading fails with an error.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import functools
+import itertools
 import os
+import threading
 from typing import Optional
 
 import numpy as np
@@ -454,6 +458,7 @@ def chunks_rebalance_step(task, chunk_off, K: int, time_per_sample):
 STATUS_BAD_ID, STATUS_TIMEOUT = 4, 8
 CLIP_WORKSPACE = 16384
 _ERR_LEN = 256
+_local = threading.local()  # the error text's buffer, one per thread
 _dtypes = None
 
 
@@ -465,6 +470,14 @@ def _types():
     return _dtypes
 
 
+def _errbuf():
+    try:
+        return _local.buf
+    except AttributeError:
+        _local.buf = C.create_string_buffer(_ERR_LEN)
+        return _local.buf
+
+
 def _dense(t, what: str) -> Dense:
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor of two dimensions" % what)
@@ -472,9 +485,10 @@ def _dense(t, what: str) -> Dense:
     if ty is None:
         raise ValueError("%s must be float32, bfloat16 or float16" % what)
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError("the rows of %s must be contiguous" % what)
-    return Dense(ty, rows, cols, t.stride(0) if rows > 1 else cols, t.data_ptr())
+    return Dense(ty, rows, cols, ld if rows > 1 else cols, t.data_ptr())
 
 
 def _vector(t, n: int, dtype, device: int, what: str) -> int:
@@ -492,31 +506,18 @@ def _status_ptr(status, device: int):
     return status.data_ptr()
 
 
-class _On:
-    """Makes the caller's stream torch's current one while outputs and workspaces are allocated."""
-
-    def __init__(self, stream: int, device: int):
-        import torch
-        self._ctx = torch.cuda.stream(torch.cuda.ExternalStream(stream, device="cuda:%d" % device))
-
-    def __enter__(self):
-        return self._ctx.__enter__()
-
-    def __exit__(self, *exc):
-        return self._ctx.__exit__(*exc)
-
-
 def _operator(fn):
-    """Adds the keyword ``stream`` to an operator."""
-    import functools
-
+    """Adds the keyword ``stream`` to an operator: the caller's stream is torch's current one while outputs and workspaces
+    are allocated and the work is enqueued."""
     @functools.wraps(fn)
-    def call(first, *args, stream: Optional[int] = None, **kw):
+    def call(*args, stream: Optional[int] = None, **kw):
         if stream is None:
-            return fn(first, *args, **kw)
-        t = first if hasattr(first, "get_device") else first[0]
-        with _On(stream, t.get_device()):
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
+        import torch
+        first = args[0] if args else next(iter(kw.values()))
+        first = first if hasattr(first, "device") else list(first)[0]
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=first.device)):
+            return fn(*args, **kw)
     return call
 
 
@@ -526,12 +527,8 @@ def _raw_stream(device: int) -> int:
 
 
 def _workspace(nbytes: int, like):
-    return like.new_empty(nbytes, dtype=_u8()) if nbytes else None
-
-
-def _u8():
     import torch
-    return torch.uint8
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
 
 def _raise(st: int, buf):
@@ -554,9 +551,8 @@ def _softmax(x, w, labels, grad: bool, weights=None, scale=1.0, status=None):
     if lib.chicle_softmax_workspace(C.byref(dx), C.byref(dw), int(grad), C.byref(need)) != OK:
         raise ChicleError(ERR_INVALID_ARG, "x and w must have one type and the same columns, w at least one row")
     ws = _workspace(need.value, x)
-    loss = torch.empty(n, dtype=torch.float32, device=x.device)
-    lse = torch.empty(n, dtype=torch.float32, device=x.device)
-    buf = C.create_string_buffer(_ERR_LEN)
+    loss, lse = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
+    buf = _errbuf()
     stream, wsp = _raw_stream(device), None if ws is None else ws.data_ptr()
     if not grad:
         _raise(lib.chicle_softmax_loss(device, stream, C.byref(dx), C.byref(dw), lp, loss.data_ptr(), lse.data_ptr(), wsp,
@@ -565,7 +561,9 @@ def _softmax(x, w, labels, grad: bool, weights=None, scale=1.0, status=None):
     gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     gw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
     _raise(lib.chicle_softmax_loss_grad(device, stream, C.byref(dx), C.byref(dw), lp, wp, scale, loss.data_ptr(), lse.data_ptr(),
-                                        C.byref(_dense(gx, "dx")), C.byref(_dense(gw, "dw")), wsp, need.value, sp, buf, _ERR_LEN), buf)
+                                        C.byref(Dense(dx.type, n, dx.cols, dx.cols, gx.data_ptr())),
+                                        C.byref(Dense(dw.type, dw.rows, dw.cols, dw.cols, gw.data_ptr())), wsp, need.value, sp, buf,
+                                        _ERR_LEN), buf)
     return loss, lse, gx, gw
 
 
@@ -595,10 +593,12 @@ def embedding(table, ids, scale: float = 1.0, out=None, status=None):
     ip = _vector(ids, n, torch.int32, device, "ids")
     if out is None:
         out = torch.empty((n, dt.cols), dtype=table.dtype, device=table.device)
+        do = Dense(dt.type, n, dt.cols, dt.cols, out.data_ptr())
     elif out.get_device() != device or out.shape[0] != n:
         raise ValueError("out must have a row per id and be on the table's device")
-    do = _dense(out, "out")
-    buf = C.create_string_buffer(_ERR_LEN)
+    else:
+        do = _dense(out, "out")
+    buf = _errbuf()
     _raise(lib.chicle_embedding(device, _raw_stream(device), C.byref(dt), ip, scale, C.byref(do), _status_ptr(status, device), buf, _ERR_LEN), buf)
     return out
 
@@ -623,7 +623,7 @@ def embedding_grad(ids, grad, rows: int, scale: float = 1.0, out=None, accumulat
     if lib.chicle_embedding_grad_workspace(dg.rows, rows, dg.cols, C.byref(need)) != OK:
         raise ChicleError(ERR_INVALID_ARG, "sizes out of range")
     ws = _workspace(need.value, grad)
-    buf = C.create_string_buffer(_ERR_LEN)
+    buf = _errbuf()
     _raise(lib.chicle_embedding_grad(device, _raw_stream(device), ip, C.byref(dg), scale, int(bool(accumulate)), C.byref(dt),
                                      None if ws is None else ws.data_ptr(), need.value, _status_ptr(status, device), buf, _ERR_LEN), buf)
     return out
@@ -634,32 +634,31 @@ def clip_gradients(tensors, max_norm: float, out=None):
     """``chicle_clip_gradients``: returns the 2-norm of all elements of all ``tensors`` (a float32 tensor without dimensions)
     and multiplies them by ``min(1, max_norm / (norm + 1e-6))``, in place or into the tensors of ``out`` (as many, of the same
     types and lengths). A norm that is not finite leaves the elements as they are. ``max_norm=inf``: the norm alone."""
-    import array
     import torch
     lib = load()
     tensors = list(tensors)
     if not tensors:
         raise ValueError("no tensors")
-    types = _types()
-    device = tensors[0].get_device()
-    kinds = [types.get(t.dtype, -1) for t in tensors]
-    lens = [t.numel() for t in tensors]
-    ins = [t.data_ptr() for t in tensors]
+    # (method by method over all tensors: a model has hundreds, and each look costs what a launch of a kernel does not)
+    T = torch.Tensor
+    device, count = tensors[0].get_device(), len(tensors)
+    kinds = list(map(_types().get, [t.dtype for t in tensors]))
+    lens, ins = list(map(T.numel, tensors)), list(map(T.data_ptr, tensors))
     # (a tensor on the host has device -1)
-    good = device >= 0 and -1 not in kinds and all([t.is_contiguous() and t.get_device() == device for t in tensors])
+    good = device >= 0 and None not in kinds and all(map(T.is_contiguous, tensors)) and set(map(T.get_device, tensors)) == {device}
     outs = ins
     if out is not None:
         out = list(out)
-        good = good and len(out) == len(tensors) and lens == [t.numel() for t in out] and kinds == [types.get(t.dtype, -1) for t in out]
-        good = good and all([t.is_contiguous() and t.get_device() == device for t in out])
-        outs = [t.data_ptr() for t in out]
+        outs = list(map(T.data_ptr, out))
+        good = (good and lens == list(map(T.numel, out)) and kinds == list(map(_types().get, [t.dtype for t in out]))
+                and all(map(T.is_contiguous, out)) and set(map(T.get_device, out)) == {device})
     if not good:
         raise ValueError("the tensors must be contiguous CUDA tensors of float32, bfloat16 or float16 on one device, and those of "
                          "out of the same number, types and lengths")
-    table = array.array("q", [v for four in zip(kinds, lens, ins, outs) for v in four])  # chicle_tensor_t: four words
-    ws = tensors[0].new_empty(CLIP_WORKSPACE, dtype=torch.uint8)
+    table = array.array("q", itertools.chain.from_iterable(zip(kinds, lens, ins, outs)))  # chicle_tensor_t: four words
+    ws = torch.empty(CLIP_WORKSPACE, dtype=torch.uint8, device=tensors[0].device)
     norm = torch.empty((), dtype=torch.float32, device=tensors[0].device)
-    buf = C.create_string_buffer(_ERR_LEN)
-    _raise(lib.chicle_clip_gradients(device, _raw_stream(device), len(tensors), table.buffer_info()[0], max_norm, norm.data_ptr(),
+    buf = _errbuf()
+    _raise(lib.chicle_clip_gradients(device, _raw_stream(device), count, table.buffer_info()[0], max_norm, norm.data_ptr(),
                                      ws.data_ptr(), CLIP_WORKSPACE, buf, _ERR_LEN), buf)
     return norm

@@ -17,16 +17,17 @@ namespace chicle {
 namespace {
 
 constexpr int kMost = 512;            // tensors per launch
-constexpr int kChunk = 8192;          // elements that a CTA takes at a time
+constexpr int kFew = 96;              // up to so many, a launch with a smaller argument
+constexpr int kChunk = 16384;         // elements that a CTA takes at a time
 constexpr int kBlocks = 148 * 8;      // CTAs, and words of workspace
 static_assert(kBlocks * sizeof(double) <= CHICLE_CLIP_WORKSPACE, "workspace");
 
-struct Table {
-    const void *in[kMost];
-    void *out[kMost];
-    int64_t n[kMost];
-    uint32_t end[kMost]; // chunks up to and with this tensor
-    uint8_t type[kMost];
+template <int M> struct Table {
+    const void *in[M];
+    void *out[M];
+    int64_t n[M];
+    uint32_t end[M]; // chunks up to and with this tensor
+    uint8_t type[M];
     int32_t count;
 };
 
@@ -36,7 +37,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(floa
 template <> __device__ __forceinline__ __half rounded<__half>(float v) { return __float2half_rn(v); }
 
 // Tensor of a chunk, and its place in it.
-__device__ __forceinline__ int tensor_of(const Table &t, uint32_t chunk, int64_t &first)
+template <int M> __device__ __forceinline__ int tensor_of(const Table<M> &t, uint32_t chunk, int64_t &first)
 {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
@@ -109,7 +110,8 @@ __device__ __forceinline__ double block_sum(double s)
     return s;
 }
 
-__global__ void __launch_bounds__(256) k_squares(const __grid_constant__ Table t, uint32_t chunks, double *__restrict__ sums, bool first)
+template <int M>
+__global__ void __launch_bounds__(256) k_squares(const __grid_constant__ Table<M> t, uint32_t chunks, double *__restrict__ sums, bool first)
 {
     double s = 0.0;
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
@@ -147,7 +149,8 @@ template <typename T> __device__ __forceinline__ void chunk_scale(const T *p, T 
     }
 }
 
-__global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table t, uint32_t chunks, const double *__restrict__ sums, int n_sums,
+template <int M>
+__global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table<M> t, uint32_t chunks, const double *__restrict__ sums, int n_sums,
                                                float max_norm, float *norm)
 {
     double s = 0.0;
@@ -167,6 +170,57 @@ __global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table t, 
             chunk_scale(static_cast<const __nv_bfloat16 *>(t.in[k]) + at, static_cast<__nv_bfloat16 *>(t.out[k]) + at, len, f);
         else chunk_scale(static_cast<const __half *>(t.in[k]) + at, static_cast<__half *>(t.out[k]) + at, len, f);
     }
+}
+
+struct Call {
+    const chicle_tensor_t *tensors;
+    int64_t count;
+    float max_norm;
+    float *norm;
+    double *sums;
+    cudaStream_t stream;
+};
+
+// Launches take up to M tensors and 2^31 chunks. Their CTAs' sums are added to the same words.
+template <int M> cudaError_t run(const Call &c)
+{
+    cudaError_t e = cudaSuccess;
+    int n_sums = 1;
+    for (int phase = 0; phase < 2 && e == cudaSuccess; ++phase) {
+        int64_t i = 0;
+        bool first = true;
+        do {
+            Table<M> t;
+            t.count = 0;
+            uint64_t chunks = 0;
+            bool any_out = false;
+            for (; i < c.count && t.count < M; ++i) {
+                const chicle_tensor_t &x = c.tensors[i];
+                if (x.n == 0) continue;
+                const uint64_t more = (uint64_t)ceil_div(x.n, kChunk);
+                if (t.count && chunks + more > 0x7fffffffu) break;
+                chunks += more;
+                t.in[t.count] = x.in;
+                t.out[t.count] = x.out;
+                t.n[t.count] = x.n;
+                t.type[t.count] = (uint8_t)x.type;
+                t.end[t.count++] = (uint32_t)chunks;
+                any_out |= x.out != nullptr;
+            }
+            const unsigned grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, kBlocks));
+            if (phase == 0) {
+                if (first) n_sums = (int)grid;
+                // (the launches behind the first keep to its words)
+                k_squares<M><<<first ? grid : std::min<unsigned>(grid, (unsigned)n_sums), 256, 0, c.stream>>>(t, (uint32_t)chunks, c.sums, first);
+                e = cudaGetLastError();
+            } else if (first || any_out) {
+                k_scale<M><<<any_out ? grid : 1, 256, 0, c.stream>>>(t, any_out ? (uint32_t)chunks : 0u, c.sums, n_sums, c.max_norm, c.norm);
+                e = cudaGetLastError();
+            }
+            first = false;
+        } while (i < c.count && e == cudaSuccess);
+    }
+    return e;
 }
 
 } // namespace
@@ -196,43 +250,7 @@ extern "C" chicle_status_t chicle_clip_gradients(int device, void *cuda_stream, 
     const DeviceGuard guard(device);
     if (!guard.ok()) return err(CHICLE_ERR_CUDA, guard.message());
     const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    double *sums = static_cast<double *>(dev_workspace);
-    // Launches take up to kMost tensors and 2^31 chunks. Their CTAs' sums are added to the same words.
-    cudaError_t e = cudaSuccess;
-    int n_sums = 1;
-    for (int phase = 0; phase < 2 && e == cudaSuccess; ++phase) {
-        int64_t i = 0;
-        bool first = true;
-        do {
-            Table t;
-            t.count = 0;
-            uint64_t chunks = 0;
-            bool any_out = false;
-            for (; i < count && t.count < kMost; ++i) {
-                const chicle_tensor_t &x = host_tensors[i];
-                if (x.n == 0) continue;
-                const uint64_t more = (uint64_t)ceil_div(x.n, kChunk);
-                if (t.count && chunks + more > 0x7fffffffu) break;
-                chunks += more;
-                t.in[t.count] = x.in;
-                t.out[t.count] = x.out;
-                t.n[t.count] = x.n;
-                t.type[t.count] = (uint8_t)x.type;
-                t.end[t.count++] = (uint32_t)chunks;
-                any_out |= x.out != nullptr;
-            }
-            const unsigned grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, kBlocks));
-            if (phase == 0) {
-                if (first) n_sums = (int)grid;
-                // (the launches behind the first keep to its words)
-                k_squares<<<first ? grid : std::min<unsigned>(grid, (unsigned)n_sums), 256, 0, s>>>(t, (uint32_t)chunks, sums, first);
-                e = cudaGetLastError();
-            } else if (first || any_out) {
-                k_scale<<<any_out ? grid : 1, 256, 0, s>>>(t, any_out ? (uint32_t)chunks : 0u, sums, n_sums, max_norm, dev_norm);
-                e = cudaGetLastError();
-            }
-            first = false;
-        } while (i < count && e == cudaSuccess);
-    }
+    const Call call{host_tensors, count, max_norm, dev_norm, static_cast<double *>(dev_workspace), s};
+    const cudaError_t e = count <= kFew ? run<kFew>(call) : run<kMost>(call);
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
 }

@@ -8,7 +8,7 @@
 // above that by radix passes of up to 10 bits. The sorted entries are cut into windows of equal length; a window sums
 // its runs of equal ids, writes those that lie inside it and leaves the ones that cross its ends as partial sums in fp32, which
 // a last kernel adds in order. So an id with most of the entries takes no longer than many ids with a few.
-// Rows without an id are zeroed by further CTAs of the same kernels.
+// Rows without an id are zeroed by further CTAs of the same launches: the sort leaves the memory idle.
 #include <algorithm>
 #include <cmath>
 
@@ -18,12 +18,15 @@ namespace chicle {
 namespace {
 
 constexpr int kMaxRankN = 4096;   // ids sorted by counting
-constexpr int kTile = 4096;       // entries per CTA of a radix pass
+constexpr int kTile = 2048;       // entries per CTA of a radix pass
 constexpr int kTileThreads = 512;
 constexpr int kDigits = 1024;
 constexpr int kGroupTiles = 32;   // tiles whose digit counts are added up in advance
 constexpr int64_t kTargetThreads = 148 * 1024;
-constexpr int64_t kZeroBytes = 128 * 1024; // of dtable per zeroing CTA
+constexpr int64_t kZeroBytes = 64 * 1024; // of dtable per zeroing CTA
+// What a launch of the sort zeroes beside it: what memory writes in the 8 to 12 us that it takes up to 10^5 entries, and in
+// the time that more take.
+constexpr int64_t kZeroShare = 48 << 20, kZeroPerEntry = 64;
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
 template <typename T> __device__ __forceinline__ T of_float(float v);
@@ -74,11 +77,45 @@ __device__ __forceinline__ int32_t key_of(int32_t id, int32_t rows, uint32_t *st
     return (uint32_t)id < (uint32_t)rows ? id : rows; // no id: behind all others
 }
 
+// Rows [v0, v1) of dtable to be zeroed, `per` of them by a CTA, in accesses of `width` bytes. `present`: a bit per row; rows
+// with an id are left out (null: none are).
+struct ZeroJob {
+    uint8_t *base;
+    int64_t pitch; // bytes
+    int32_t row_bytes, width, per;
+    int64_t v0, v1;
+    const uint32_t *present;
+    __host__ __device__ int64_t blocks() const { return v1 > v0 ? (v1 - v0 + per - 1) / per : 0; }
+};
+
+template <typename W> __device__ __forceinline__ void zero_rows(const ZeroJob &z, int64_t block)
+{
+    const int pieces = z.row_bytes / (int)sizeof(W);
+    int log = 0;
+    while ((1 << log) < pieces && (2 << log) <= (int)blockDim.x) ++log; // threads per row
+    const int64_t v0 = z.v0 + block * z.per, v1 = min(v0 + z.per, z.v1);
+    for (int64_t v = v0 + (threadIdx.x >> log); v < v1; v += blockDim.x >> log) {
+        if (z.present && ((z.present[v >> 5] >> (v & 31)) & 1u)) continue;
+        W *row = reinterpret_cast<W *>(z.base + v * z.pitch);
+#pragma unroll 4
+        for (int c = threadIdx.x & ((1 << log) - 1); c < pieces; c += 1 << log) row[c] = W{};
+    }
+}
+
+__device__ __forceinline__ void zero_block(const ZeroJob &z, int64_t block)
+{
+    if (z.width == 16) zero_rows<uint4>(z, block);
+    else if (z.width == 8) zero_rows<uint2>(z, block);
+    else if (z.width == 4) zero_rows<uint32_t>(z, block);
+    else zero_rows<uint16_t>(z, block);
+}
+
 // Place of every id in the sorted order: the number of smaller ones, and of equal ones in front of it. 32 ids per CTA,
 // eight threads each count an eighth.
 __global__ void __launch_bounds__(256) k_rank_ids(const int32_t *__restrict__ ids, int32_t n, int32_t rows, int32_t *__restrict__ keys,
-                                                  int32_t *__restrict__ order, uint32_t *status)
+                                                  int32_t *__restrict__ order, uint32_t *status, const ZeroJob zero)
 {
+    if ((int64_t)blockIdx.x * 32 >= n) return zero_block(zero, (int64_t)blockIdx.x - (n + 31) / 32);
     __shared__ __align__(16) int32_t s_key[kMaxRankN];
     __shared__ int s_part[8][32];
     const int padded = (n + 31) & ~31;
@@ -108,9 +145,11 @@ __global__ void __launch_bounds__(256) k_rank_ids(const int32_t *__restrict__ id
 // Digit counts of a tile: its own row of `hist`, and added to its group's row and to the total.
 __global__ void __launch_bounds__(kTileThreads) k_id_hist(const int32_t *__restrict__ in, int64_t n, int32_t rows, bool raw, int shift, int digits,
                                                           uint32_t *__restrict__ hist, uint32_t *__restrict__ group,
-                                                          uint32_t *__restrict__ total, uint32_t *status)
+                                                          uint32_t *__restrict__ total, uint32_t *present, uint32_t *status,
+                                                          const ZeroJob zero)
 {
     __shared__ uint32_t h[kDigits];
+    if ((int64_t)blockIdx.x * kTile >= n) return zero_block(zero, (int64_t)blockIdx.x - (n + kTile - 1) / kTile);
     for (int j = threadIdx.x; j < digits; j += kTileThreads) h[j] = 0;
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kTile;
@@ -119,6 +158,10 @@ __global__ void __launch_bounds__(kTileThreads) k_id_hist(const int32_t *__restr
         const int64_t i = base + it * kTileThreads + threadIdx.x;
         const bool live = i < n;
         const int32_t k = live ? (raw ? key_of(in[i], rows, status) : in[i]) : 0;
+        if (live && present && k < rows) { // (looked at first: a frequent id's word would queue up its atomics)
+            const uint32_t bit = 1u << (k & 31);
+            if (!(__ldcg(&present[k >> 5]) & bit)) atomicOr(&present[k >> 5], bit);
+        }
         const int dg = live ? (k >> shift) & (digits - 1) : -1;
         // one atomic per digit of a warp: a frequent id would queue up
         const uint32_t peers = __match_any_sync(0xffffffffu, dg);
@@ -139,8 +182,9 @@ __global__ void __launch_bounds__(kTileThreads) k_id_hist(const int32_t *__restr
 __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__restrict__ in, const int32_t *__restrict__ order_in, int64_t n,
                                                              int32_t rows, bool raw, int shift, int digits, const uint32_t *__restrict__ hist,
                                                              const uint32_t *__restrict__ group, const uint32_t *__restrict__ total,
-                                                             int32_t *__restrict__ keys, int32_t *__restrict__ order)
+                                                             int32_t *__restrict__ keys, int32_t *__restrict__ order, const ZeroJob zero)
 {
+    if ((int64_t)blockIdx.x * kTile >= n) return zero_block(zero, (int64_t)blockIdx.x - (n + kTile - 1) / kTile);
     constexpr int kWarps = kTileThreads / 32, kItems = kTile / kTileThreads;
     extern __shared__ uint32_t smem[];
     uint32_t(*cnt)[kDigits] = reinterpret_cast<uint32_t(*)[kDigits]>(smem); // [warp][digit]
@@ -177,7 +221,9 @@ __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__re
         tot[k] = own[k] = 0;
         if (d < digits) {
             tot[k] = total[d];
+#pragma unroll 8
             for (int j = 0; j < g; ++j) own[k] += group[(int64_t)j * digits + d];
+#pragma unroll 8
             for (int j = g * kGroupTiles; j < (int)blockIdx.x; ++j) own[k] += hist[(int64_t)j * digits + d];
         }
     }
@@ -246,7 +292,7 @@ struct Sums {
     float scale;
     int accumulate;
     float *partial;       // [window][2][d]: of the run that came in, of the run that goes out
-    int64_t sum_blocks, zero_rows; // CTAs that sum, rows per zeroing CTA
+    int64_t sum_blocks;   // CTAs that sum; the others zero
 };
 
 template <typename T, int E>
@@ -274,37 +320,10 @@ template <int E> __device__ __forceinline__ void put_partial(const Sums &s, int6
 }
 
 template <typename T, int E>
-__global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__restrict__ grad, int64_t ld, T *__restrict__ table, int64_t ld_t)
+__global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__restrict__ grad, int64_t ld, T *__restrict__ table, int64_t ld_t,
+                                                   const ZeroJob zero)
 {
-    if (blockIdx.x >= s.sum_blocks) {
-        // rows without an id
-        __shared__ uint32_t s_has[32];
-        const int64_t v0 = (int64_t)(blockIdx.x - s.sum_blocks) * s.zero_rows, v1 = min(v0 + s.zero_rows, (int64_t)s.rows);
-        __shared__ int32_t s_first;
-        if (threadIdx.x < 32) {
-            s_has[threadIdx.x] = 0;
-            const int32_t f = first_not_below(s.keys, (int32_t)s.n, (int32_t)v0);
-            if (threadIdx.x == 0) s_first = f;
-        }
-        __syncthreads();
-        for (int64_t e = s_first + (int64_t)threadIdx.x; e < s.n; e += 256) {
-            const int32_t k = s.keys[e];
-            if (k >= v1) break;
-            const int b = (int)(k - v0);
-            if (e == 0 || s.keys[e - 1] != k) atomicOr(&s_has[b >> 5], 1u << (b & 31));
-        }
-        __syncthreads();
-        Vec<T, E> none;
-#pragma unroll
-        for (int j = 0; j < E; ++j) none.v[j] = of_float<T>(0.f);
-        for (int64_t v = v0 + (threadIdx.x >> s.tpr_log); v < v1; v += 256 >> s.tpr_log) {
-            const int b = (int)(v - v0);
-            if ((s_has[b >> 5] >> (b & 31)) & 1u) continue;
-            Vec<T, E> *row = reinterpret_cast<Vec<T, E> *>(table + v * ld_t);
-            for (int c = threadIdx.x & ((1 << s.tpr_log) - 1); c < s.vecs; c += 1 << s.tpr_log) row[c] = none;
-        }
-        return;
-    }
+    if (blockIdx.x >= s.sum_blocks) return zero_block(zero, (int64_t)blockIdx.x - s.sum_blocks);
     const int tpr = 1 << s.tpr_log, per = 256 >> s.tpr_log;
     const int64_t slab = blockIdx.x % s.slabs, wb = blockIdx.x / s.slabs;
     const int c = (int)slab * tpr + (threadIdx.x & (tpr - 1));
@@ -318,12 +337,15 @@ __global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__rest
     for (int j = 0; j < E; ++j) acc[j] = 0.f;
     constexpr int kAhead = 8;
     for (int64_t e = e0; e < e1; e += kAhead) {
-        int32_t key[kAhead];
+        // (windows begin at multiples of 8; the arrays have room behind the last entry)
+        const Vec<int32_t, 8> at = *reinterpret_cast<const Vec<int32_t, 8> *>(s.order + e);
+        Vec<int32_t, 8> keys = *reinterpret_cast<const Vec<int32_t, 8> *>(s.keys + e);
+        int32_t(&key)[kAhead] = keys.v;
         Vec<T, E> q[kAhead];
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            key[a] = e + a < e1 ? s.keys[e + a] : s.rows;
-            if (key[a] < s.rows) q[a] = *reinterpret_cast<const Vec<T, E> *>(grad + (int64_t)s.order[e + a] * ld + (int64_t)c * E);
+            if (e + a >= e1) key[a] = s.rows;
+            if (key[a] < s.rows) q[a] = *reinterpret_cast<const Vec<T, E> *>(grad + (int64_t)at.v[a] * ld + (int64_t)c * E);
         }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
@@ -352,43 +374,79 @@ __global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__rest
     }
 }
 
-// Adds the partial sums of runs that cross windows: the CTA of the window where a run begins. Its groups of threads
-// take consecutive windows each, and their sums are added in order.
+// Adds the partial sums of the runs that cross windows, in order. A warp looks at the window where a run may begin; it adds
+// a few partial sums itself, many are left to the CTA: its groups of threads take consecutive windows each, and their
+// sums are added in order.
+constexpr int kWarpJoin = 32; // partial sums that a warp takes
+
 template <typename T, int E>
 __global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restrict__ table, int64_t ld_t)
 {
     __shared__ float s_sum[256][E];
-    const int64_t w = blockIdx.x;
-    const int64_t e0 = w * s.window, e1 = min(e0 + s.window, s.n);
-    if (e1 >= s.n) return;
-    const int32_t k = s.keys[e1];
-    if (s.keys[e1 - 1] != k || k >= s.rows) return;
-    if (s.keys[e0] == k && e0 > 0 && s.keys[e0 - 1] == k) return; // begins in an earlier window
-    const int64_t end = first_not_below(s.keys + e1, (int32_t)(s.n - e1), k + 1) + e1;
-    const int64_t last = (end - 1) / s.window; // windows w + 1 .. last hold the rest
-    const int tpr = 1 << s.tpr_log, groups = 256 >> s.tpr_log;
-    const int c = blockIdx.y * tpr + (threadIdx.x & (tpr - 1)), g = threadIdx.x >> s.tpr_log;
-    const int64_t count = last - w + 1;
-    float acc[E];
+    __shared__ int64_t s_count[8];
+    __shared__ int32_t s_key[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tpr = 1 << s.tpr_log;
+    const int c_end = min(s.vecs, ((int)blockIdx.y + 1) * tpr), c_begin = (int)blockIdx.y * tpr;
+    const int64_t w0 = (int64_t)blockIdx.x * 8;
+    int64_t count = 0;
+    {
+        const int64_t w = w0 + warp;
+        const int64_t e0 = w * s.window, e1 = e0 + s.window;
+        if (e1 < s.n) {
+            const int32_t k = s.keys[e1], last = s.keys[e1 - 1], first = s.keys[e0], before = e0 > 0 ? s.keys[e0 - 1] : -1;
+            if (last == k && k < s.rows && !(first == k && before == k)) {
+                // windows w + 1 .. the one with the run's last entry hold the rest
+                const int64_t end = first_not_below(s.keys + e1, (int32_t)(s.n - e1), k + 1) + e1;
+                count = (end - 1) / s.window - w + 1;
+                if (count <= kWarpJoin) {
+                    for (int c = c_begin + lane; c < c_end; c += 32) {
+                        float acc[E];
 #pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] = 0.f;
-    if (c < s.vecs) {
-        const int64_t a = count * g / groups, b = count * (g + 1) / groups;
-#pragma unroll 8
-        for (int64_t i = a; i < b; ++i) {
-            const Vec<float, E> p = *reinterpret_cast<const Vec<float, E> *>(s.partial + ((w + i) * 2 + (i == 0 ? 1 : 0)) * s.d + (int64_t)c * E);
+                        for (int j = 0; j < E; ++j) acc[j] = 0.f;
+#pragma unroll 4
+                        for (int64_t i = 0; i < count; ++i) {
+                            const Vec<float, E> p = *reinterpret_cast<const Vec<float, E> *>(s.partial + ((w + i) * 2 + (i == 0 ? 1 : 0)) * s.d + (int64_t)c * E);
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] += p.v[j];
+                            for (int j = 0; j < E; ++j) acc[j] += p.v[j];
+                        }
+                        put_row<T, E>(s, table, ld_t, k, c, acc);
+                    }
+                    count = 0;
+                }
+                if (lane == 0) s_key[warp] = k;
+            }
         }
     }
-#pragma unroll
-    for (int j = 0; j < E; ++j) s_sum[threadIdx.x][j] = acc[j];
+    if (lane == 0) s_count[warp] = count;
     __syncthreads();
-    if (g == 0 && c < s.vecs) {
-        for (int o = 1; o < groups; ++o)
+    const int groups = 256 >> s.tpr_log, g = threadIdx.x >> s.tpr_log, c = c_begin + (threadIdx.x & (tpr - 1));
+    for (int i = 0; i < 8; ++i) {
+        count = s_count[i];
+        if (count == 0) continue; // (the same for all threads)
+        const int64_t w = w0 + i;
+        float acc[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] += s_sum[threadIdx.x + (o << s.tpr_log)][j];
-        put_row<T, E>(s, table, ld_t, k, c, acc);
+        for (int j = 0; j < E; ++j) acc[j] = 0.f;
+        if (c < c_end) {
+            const int64_t a = count * g / groups, b = count * (g + 1) / groups;
+#pragma unroll 8
+            for (int64_t q = a; q < b; ++q) {
+                const Vec<float, E> p = *reinterpret_cast<const Vec<float, E> *>(s.partial + ((w + q) * 2 + (q == 0 ? 1 : 0)) * s.d + (int64_t)c * E);
+#pragma unroll
+                for (int j = 0; j < E; ++j) acc[j] += p.v[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) s_sum[threadIdx.x][j] = acc[j];
+        __syncthreads();
+        if (g == 0 && c < c_end) {
+            for (int o = 1; o < groups; ++o)
+#pragma unroll
+                for (int j = 0; j < E; ++j) acc[j] += s_sum[threadIdx.x + (o << s.tpr_log)][j];
+            put_row<T, E>(s, table, ld_t, s_key[i], c, acc);
+        }
+        __syncthreads();
     }
 }
 
@@ -405,7 +463,7 @@ struct IdPlan {
     int passes = 0, digit_bits = 0;
     int64_t tiles = 0, groups = 0;
     int64_t window = 0, windows = 0;
-    size_t keys[2], order[2], hist, group, total, partial, bytes; // offsets; group and total of all passes lie together
+    size_t keys[2], order[2], hist, group, total, present, partial, bytes; // offsets; what has to begin at zero lies together
     size_t zero_at, zero_bytes;
 };
 
@@ -425,8 +483,8 @@ IdPlan make_plan(int64_t n, int64_t rows, int64_t cols)
     while (p.window < 4096 && ceil_div(n, p.window) > want) p.window *= 2;
     p.windows = ceil_div(n, p.window);
     for (int k = 0; k < 2; ++k) {
-        p.keys[k] = take((size_t)n * 4);
-        p.order[k] = take((size_t)n * 4);
+        p.keys[k] = take((size_t)n * 4 + 32); // (read in eights)
+        p.order[k] = take((size_t)n * 4 + 32);
     }
     if (n > kMaxRankN) {
         const int bits = log2_up(rows + 1);
@@ -439,6 +497,7 @@ IdPlan make_plan(int64_t n, int64_t rows, int64_t cols)
         p.zero_at = at;
         p.group = take((size_t)p.passes * p.groups * digits * 4);
         p.total = take((size_t)p.passes * digits * 4);
+        p.present = take((size_t)ceil_div(rows, 32) * 4);
         p.zero_bytes = at - p.zero_at;
     }
     p.partial = take((size_t)p.windows * 2 * cols * 4);
@@ -446,29 +505,45 @@ IdPlan make_plan(int64_t n, int64_t rows, int64_t cols)
     return p;
 }
 
-// Sorted keys and order are in buffer `which` afterwards.
-cudaError_t sort_ids(const IdPlan &p, const int32_t *ids, int64_t n, int32_t rows, uint8_t *ws, uint32_t *status, cudaStream_t s, int *which)
+// Sorted keys and order are in buffer `which` afterwards. Takes its share of the rows to be zeroed off `zero`.
+cudaError_t sort_ids(const IdPlan &p, const int32_t *ids, int64_t n, int32_t rows, uint8_t *ws, uint32_t *status, cudaStream_t s, int *which,
+                     ZeroJob *zero)
 {
     int32_t *keys[2] = {reinterpret_cast<int32_t *>(ws + p.keys[0]), reinterpret_cast<int32_t *>(ws + p.keys[1])};
     int32_t *order[2] = {reinterpret_cast<int32_t *>(ws + p.order[0]), reinterpret_cast<int32_t *>(ws + p.order[1])};
     *which = 0;
     if (n <= kMaxRankN) {
-        k_rank_ids<<<(unsigned)ceil_div(n, 32), 256, 0, s>>>(ids, (int32_t)n, rows, keys[0], order[0], status);
+        // (a few thousand rows at most are written twice)
+        const int64_t blocks = ceil_div(n, 32) + zero->blocks();
+        k_rank_ids<<<(unsigned)blocks, 256, 0, s>>>(ids, (int32_t)n, rows, keys[0], order[0], status, *zero);
+        zero->v0 = zero->v1;
         return cudaGetLastError();
     }
     constexpr int kSmem = kTileThreads / 32 * kDigits * 4;
     cudaError_t e = cudaFuncSetAttribute(k_id_scatter, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e == cudaSuccess) e = cudaMemsetAsync(ws + p.zero_at, 0, p.zero_bytes, s);
     const int digits = 1 << p.digit_bits;
+    const int64_t share = std::max<int64_t>(1, (kZeroShare + kZeroPerEntry * n) / zero->row_bytes);
+    auto part = [&] { // the next launch's share, in whole words of `present`
+        ZeroJob z = *zero;
+        z.v1 = std::min(z.v1, (z.v0 + share + 31) / 32 * 32);
+        zero->v0 = z.v1;
+        return z;
+    };
+    uint32_t *present = zero->blocks() ? reinterpret_cast<uint32_t *>(ws + p.present) : nullptr;
     for (int k = 0; e == cudaSuccess && k < p.passes; ++k) {
         const bool raw = k == 0;
         const int32_t *in = raw ? ids : keys[(k + 1) & 1];
         uint32_t *hist = reinterpret_cast<uint32_t *>(ws + p.hist);
         uint32_t *group = reinterpret_cast<uint32_t *>(ws + p.group) + (size_t)k * p.groups * digits;
         uint32_t *total = reinterpret_cast<uint32_t *>(ws + p.total) + (size_t)k * digits;
-        k_id_hist<<<(unsigned)p.tiles, kTileThreads, 0, s>>>(in, n, rows, raw, k * p.digit_bits, digits, hist, group, total, status);
-        k_id_scatter<<<(unsigned)p.tiles, kTileThreads, kSmem, s>>>(in, order[(k + 1) & 1], n, rows, raw, k * p.digit_bits, digits, hist, group,
-                                                                    total, keys[k & 1], order[k & 1]);
+        ZeroJob z = part();
+        k_id_hist<<<(unsigned)(p.tiles + z.blocks()), kTileThreads, 0, s>>>(in, n, rows, raw, k * p.digit_bits, digits, hist, group, total,
+                                                                            raw ? present : nullptr, status, z);
+        if (raw) zero->present = present; // known from here on
+        z = part();
+        k_id_scatter<<<(unsigned)(p.tiles + z.blocks()), kTileThreads, kSmem, s>>>(in, order[(k + 1) & 1], n, rows, raw, k * p.digit_bits, digits, hist,
+                                                                                   group, total, keys[k & 1], order[k & 1], z);
         e = cudaGetLastError();
         *which = k & 1;
     }
@@ -506,18 +581,16 @@ cudaError_t lookup(const chicle_dense_t &t, const int32_t *ids, float scale, con
 }
 
 template <typename T, int E>
-cudaError_t sum_by_id(Sums sm, const chicle_dense_t &g, const chicle_dense_t &t, cudaStream_t s)
+cudaError_t sum_by_id(Sums sm, const chicle_dense_t &g, const chicle_dense_t &t, const ZeroJob &zero, cudaStream_t s)
 {
     sm.vecs = (int)(g.cols / E);
     sm.tpr_log = std::min(8, log2_up(sm.vecs));
     sm.slabs = (int)ceil_div(sm.vecs, 1 << sm.tpr_log);
     sm.sum_blocks = ceil_div(sm.windows, 256 >> sm.tpr_log) * sm.slabs;
-    sm.zero_rows = std::max<int64_t>(1, std::min<int64_t>(1024, kZeroBytes / (g.cols * size_of(g.type))));
-    const int64_t zero_blocks = sm.accumulate ? 0 : ceil_div(sm.rows, sm.zero_rows);
-    k_sum_by_id<T, E><<<(unsigned)(sm.sum_blocks + zero_blocks), 256, 0, s>>>(sm, (const T *)g.data, g.ld, (T *)t.data, t.ld);
+    k_sum_by_id<T, E><<<(unsigned)(sm.sum_blocks + zero.blocks()), 256, 0, s>>>(sm, (const T *)g.data, g.ld, (T *)t.data, t.ld, zero);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && sm.windows > 1) {
-        k_join_windows<T, E><<<dim3((unsigned)sm.windows, (unsigned)sm.slabs), 256, 0, s>>>(sm, (T *)t.data, t.ld);
+        k_join_windows<T, E><<<dim3((unsigned)ceil_div(sm.windows, 8), (unsigned)sm.slabs), 256, 0, s>>>(sm, (T *)t.data, t.ld);
         e = cudaGetLastError();
     }
     return e;
@@ -611,7 +684,14 @@ extern "C" chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, 
     }
     uint8_t *ws = static_cast<uint8_t *>(dev_workspace);
     int which = 0;
-    e = sort_ids(p, dev_ids, n, (int32_t)dtable->rows, ws, dev_status, s, &which);
+    ZeroJob zero{};
+    zero.base = static_cast<uint8_t *>(dtable->data);
+    zero.row_bytes = (int32_t)(dtable->cols * size_of(dtable->type));
+    zero.pitch = dtable->ld * size_of(dtable->type);
+    zero.width = vector_elements(*dtable, *dtable) * size_of(dtable->type);
+    zero.per = (int32_t)std::max<int64_t>(1, kZeroBytes / zero.row_bytes);
+    zero.v1 = accumulate ? 0 : dtable->rows;
+    e = sort_ids(p, dev_ids, n, (int32_t)dtable->rows, ws, dev_status, s, &which, &zero);
     if (e == cudaSuccess) {
         Sums sm{};
         sm.keys = reinterpret_cast<int32_t *>(ws + p.keys[which]);
@@ -621,7 +701,7 @@ extern "C" chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, 
         sm.scale = scale, sm.accumulate = accumulate;
         sm.partial = reinterpret_cast<float *>(ws + p.partial);
         e = by_type(grad->type, vector_elements(*grad, *dtable), [&](auto tag, auto width) {
-            return sum_by_id<decltype(tag), decltype(width)::value>(sm, *grad, *dtable, s);
+            return sum_by_id<decltype(tag), decltype(width)::value>(sm, *grad, *dtable, zero, s);
         });
     }
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);

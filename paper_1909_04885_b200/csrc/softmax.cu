@@ -4,16 +4,16 @@
 //   l_iv = x_i . w_v        lse_i = log sum_v exp(l_iv)        loss_i = lse_i - l_{i, y_i}
 //   p_iv = g_i (exp(l_iv - lse_i) - [v = y_i])                 dX = P W,  dW = P^T X
 //
-// The logits are never held as a whole. The loss alone keeps, per row and 128 classes, the largest logit and the sum of
-// exponentials relative to it; a second kernel joins them. For the gradients the rows are taken in pieces of about a
-// gigabyte of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the largest of the row in 128
+// The logits are never held as a whole. The loss alone keeps, per row and 128 (or 64) classes, the largest logit and the sum
+// of exponentials relative to it; a second kernel joins them. For the gradients the rows are taken in pieces of about two
+// gigabytes of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the largest of the row in its 128
 // classes) as fp16, scaled by 2^15 so that what is 2^-29 of the tile's largest still has all its bits; an elementwise
 // pass turns the piece into P in place, and two products take dX and the piece's share of dW from it. So the
 // logits are computed once: 6 n V d operations, against 8 where they are computed again for the gradient, for 6 bytes of traffic
 // per logit (at d = 4096 a third of the products' time against a twentieth).
 //
-// Rounding: logits, sums and gradients in fp32; P is rounded once to the operands' type (fp16: scaled so that the
-// largest weight comes to 2^14), and the entry of the label comes from expm1(-loss), not from a difference.
+// Rounding: logits, sums and gradients in fp32; P is rounded once to the operands' type (fp16: scaled so that the largest
+// weight comes to 2^14 and more; single precision: to two fp16 planes, tensor_core.cuh), and the entry of the label comes from expm1(-loss), not from a difference.
 #include <algorithm>
 #include <cmath>
 
@@ -25,106 +25,129 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kStoreScale = 32768.f; // fp16 exponentials are held times 2^15
-constexpr int kHalfTile = 128;         // classes per pair of (largest, sum)
+
+// Two floats in one register pair: sm_100 adds and multiplies them in one instruction.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return (uint64_t)__float_as_uint(lo) | ((uint64_t)__float_as_uint(hi) << 32); }
+__device__ __forceinline__ float low_of(uint64_t p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float high_of(uint64_t p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 2^x, off by 2^-22 of itself; what would be subnormal is 0.
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Powers of two in device memory: of P (its largest weight comes to [2^14, 2^15)), X and W (their largest elements do), and their
+// inverses. P is scaled wherever it is held in fp16, X and W in single precision.
+enum { kLift, kInvLift, kLiftX, kInvX, kLiftW, kInvW, kScales };
 
 // ---- epilogues ---------------------------------------------------------------------------------------------
 
-// Reduces a tile of logits to (largest, sum of exponentials) per row and 128 classes, keeps the label's logit, and
+// Reduces a tile of logits to (largest, sum of exponentials) per row and N classes, keeps the label's logit, and
 // writes the exponentials for the gradients: StoreT void (loss alone), half, or float (single precision).
 template <typename StoreT> struct LogitsEpilogue {
+    static constexpr bool kStream = false;
     const int32_t *labels; // rows of this piece
-    float2 *stats;         // [128-class block][rows]
+    float2 *stats;         // [block of N classes][rows]
     float *label_logit;    // [rows]
     StoreT *store;         // [rows][ld]
     int64_t ld;
+    const float *scales;   // single precision: the operands' scales (Scales); else null
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const tc::Shape &s, const tc::Tile &, int row0, int col0, uint32_t tmem, int quarter,
-                                         int half, int lane) const
+    template <int N>
+    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, uint32_t (&r)[N],
+                                           uint8_t *patch) const
     {
-        static_assert(BN == 2 * kHalfTile, "a warp takes 128 classes");
-        const int row = row0 + quarter * 32 + lane;
-        const int c0 = col0 + half * kHalfTile;
-        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * kHalfTile);
+        const int row = row0 + lane;
         const bool live = row < s.m;
+        const float factor = scales ? scales[kInvX] * scales[kInvW] : 1.f; // of an accumulator, to a logit
         const int lab = live ? labels[row] - c0 : -1; // (a negative label is in front of every block)
-        uint32_t r[32];
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int c = 0; c < kHalfTile; c += 32) {
-            if (c0 + c >= s.n) break;
-            tc::load32(at + c, r);
-            tc::wait_loads();
-            if (c0 + c + 32 > s.n) {
+        if (c0 + N > end) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c0 + c + j >= s.n) r[j] = 0xff800000u;
-            }
-            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int j = 0; j < 32; ++j) t[j & 3] = fmaxf(t[j & 3], __uint_as_float(r[j]));
-            top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-            if (lab >= c && lab < c + 32) {
-                float v = 0.f;
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (lab - c == j) v = __uint_as_float(r[j]);
-                label_logit[row] = v;
-            }
-            __syncwarp();
+            for (int j = 0; j < N; ++j)
+                if (c0 + j >= end) r[j] = 0xff800000u; // -inf
         }
+        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < N; ++j) t[j & 3] = fmaxf(t[j & 3], __uint_as_float(r[j]));
+        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+#pragma unroll
+        for (int g = 0; g < N; g += 32)
+            if ((uint32_t)(lab - g) < 32u && c0 + lab < end) { // one of 32 registers by the bits of its number
+                uint32_t q[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) q[j] = (lab & 16) ? r[g + 16 + j] : r[g + j];
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+                    for (int j = 0; j < w; ++j) q[j] = (lab & w) ? q[w + j] : q[j];
+                label_logit[row] = __uint_as_float(q[0]) * factor;
+            }
         // (a block without a logit above -inf: relative to 0, so that its exponentials are 0 and not NaN)
         const float ref = top == -INFINITY ? 0.f : top;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-        for (int c = 0; c < kHalfTile; c += 32) {
-            if (c0 + c >= s.n) break;
-            tc::load32(at + c, r);
-            tc::wait_loads();
-            if (c0 + c + 32 > s.n) {
+        uint64_t sum[2] = {0, 0}; // pairs of floats
+        const uint64_t back = pair_of(-ref, -ref), to_log2 = pair_of(kLog2e * factor, kLog2e * factor);
+        constexpr int kWidth = sizeof(StoreT) >= 2 ? 128 / (int)sizeof(StoreT) : N; // columns of a patch
+        constexpr int kPer = sizeof(StoreT) >= 2 ? 16 / (int)sizeof(StoreT) : 8;    // and of a piece
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c0 + c + j >= s.n) r[j] = 0xff800000u;
-            }
-            float e[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                e[j] = exp2f((__uint_as_float(r[j]) - ref) * kLog2e);
-                sum[j & 3] += e[j];
-            }
-            if constexpr (sizeof(StoreT) == 2) {
-                if (live) {
-                    uint4 *dst = reinterpret_cast<uint4 *>(store + (int64_t)row * ld + c0 + c);
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        if (c0 + c + j < s.n) { // (ld: a multiple of 8, what lies behind the last class is not read)
-                            uint4 q;
-                            __half2 *h = reinterpret_cast<__half2 *>(&q);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                h[i] = __floats2half2_rn(e[j + 2 * i] * kStoreScale, e[j + 2 * i + 1] * kStoreScale);
-                            dst[j / 8] = q;
-                        }
-                    }
-                }
-            } else if constexpr (sizeof(StoreT) == 4) {
-                if (live) {
-                    float4 *dst = reinterpret_cast<float4 *>(store + (int64_t)row * ld + c0 + c);
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        if (c0 + c + j < s.n) dst[j / 4] = make_float4(e[j], e[j + 1], e[j + 2], e[j + 3]);
-                }
-            }
+        for (int g = 0; g < N; g += kWidth) {
             __syncwarp();
+#pragma unroll
+            for (int c = 0; c < kWidth; c += kPer) {
+                float e[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; j += 2) {
+                    // (the difference first: it is exact where it matters, the logarithm's product is not)
+                    const uint64_t z = mul2(add2(pair_of(__uint_as_float(r[g + c + j]), __uint_as_float(r[g + c + j + 1])), back), to_log2);
+                    e[j] = exp2_of(low_of(z));
+                    e[j + 1] = exp2_of(high_of(z));
+                    sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pair_of(e[j], e[j + 1]));
+                }
+                if constexpr (sizeof(StoreT) == 2) {
+                    uint4 q;
+                    __half2 *h = reinterpret_cast<__half2 *>(&q);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(e[2 * i] * kStoreScale, e[2 * i + 1] * kStoreScale);
+                    *tc::patch_at(patch, lane, c / kPer) = q;
+                } else if constexpr (sizeof(StoreT) == 4) {
+                    *reinterpret_cast<float4 *>(tc::patch_at(patch, lane, c / kPer)) = make_float4(e[0], e[1], e[2], e[3]);
+                }
+            }
+            if constexpr (sizeof(StoreT) >= 2) {
+                __syncwarp();
+                const int piece = lane & 7, col = c0 + g + piece * kPer;
+                StoreT *dst = store + (int64_t)(row0 + (lane >> 3)) * ld + col;
+#pragma unroll 2
+                for (int i = 0; i < 8; ++i) { // (ld: a multiple of 8, what lies behind the last class is not read)
+                    const int rr = 4 * i + (lane >> 3);
+                    if (row0 + rr < s.m && col < end) *reinterpret_cast<uint4 *>(dst + (int64_t)(4 * i) * ld) = *tc::patch_at(patch, rr, piece);
+                }
+            }
         }
         // NaN: fmaxf passes over it, the sum does not
-        if (live && c0 < s.n) stats[(int64_t)(c0 / kHalfTile) * s.m + row] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+        // (blocks: two per tile, whether the second has columns or not)
+        if (live && c0 < end) stats[(int64_t)(tl.n * 2 + (c0 - tl.n * s.cols >= N)) * s.m + row] = make_float2(top * factor, (low_of(sum[0]) + low_of(sum[1])) + (high_of(sum[0]) + high_of(sum[1])));
     }
 };
 
 struct NoStore {
     char c;
 };
+
+__device__ __forceinline__ float factor_of(const float *a, const float *b) { return (a ? *a : 1.f) * (b ? *b : 1.f); }
 
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
@@ -134,118 +157,114 @@ template <> __device__ __forceinline__ __half from_float<__half>(float v) { retu
 // Where a tile of a gradient goes. With splits: to `partial`, one plane per split. Else sum = (add ? *add : 0) + tile; to
 // `keep` (fp32, for the pieces that follow) or to `out`.
 template <typename OutT> struct GradEpilogue {
+    static constexpr bool kStream = sizeof(OutT) == 2; // single precision: sums in chunks
     OutT *out;
     int64_t ld;
     float *partial;          // [split][m][n]
     const float *add;        // [m][n], or null
     float *keep;             // [m][n], or null
-    const float *scale;      // device factor of the result, or null
+    const float *scale, *scale_b; // device factors of the result, or null
     const int32_t *labels;   // rows without a label come out 0 whatever the other operand holds; or null
     int32_t classes;
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const tc::Shape &s, const tc::Tile &tl, int row0, int col0, uint32_t tmem, int quarter,
-                                         int half, int lane) const
+    template <int N>
+    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, uint32_t (&r)[N],
+                                           uint8_t *patch) const
     {
-        const int row = row0 + quarter * 32 + lane;
-        const int c0 = col0 + half * (BN / 2);
-        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * (BN / 2));
-        const bool live = row < s.m;
         const bool whole = partial || keep;
-        const float f = whole || !scale ? 1.f : *scale;
-        const bool zero = live && labels && ((uint32_t)labels[row] >= (uint32_t)classes);
-        float *dst32 = partial ? partial + ((int64_t)tl.split * s.m + row) * s.n : keep + (int64_t)row * s.n;
+        const float f = whole ? 1.f : factor_of(scale, scale_b);
+        const uint32_t zeros = __ballot_sync(0xffffffffu, labels && row0 + lane < s.m && (uint32_t)labels[row0 + lane] >= (uint32_t)classes);
+        float *dst32 = partial ? partial + (int64_t)tl.split * s.m * s.n : keep;
+        const float *src = partial ? nullptr : add;
         const bool quads = (s.n & 3) == 0; // fp32 rows of n: 16-byte pieces
-        uint32_t r[32];
-#pragma unroll 1
-        for (int c = 0; c < BN / 2; c += 32) {
-            const int col = c0 + c;
-            if (col >= s.n) break;
-            tc::load32(at + c, r);
-            tc::wait_loads();
-            if (live) finish(s, row, col, r, zero, whole, f, quads, dst32);
+        const bool quads_out = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * sizeof(OutT))) & (4 * sizeof(OutT) - 1)) == 0;
+#pragma unroll
+        for (int g = 0; g < N; g += 32) {
+            if (c0 + g >= end) break;
             __syncwarp();
-        }
-    }
-
-    __device__ __forceinline__ void finish(const tc::Shape &s, int row, int col, const uint32_t (&r)[32], bool zero, bool whole, float f,
-                                           bool quads, float *dst32) const
-    {
-        float v[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = zero ? 0.f : __uint_as_float(r[j]);
-        const bool full = col + 32 <= s.n;
-        if (add && !partial) {
-            const float *src = add + (int64_t)row * s.n + col;
-            if (full && quads) {
+            for (int c = 0; c < 8; ++c) *tc::patch_at(patch, lane, c) = make_uint4(r[g + 4 * c], r[g + 4 * c + 1], r[g + 4 * c + 2], r[g + 4 * c + 3]);
+            __syncwarp();
+            const int col = c0 + g + 4 * (lane & 7);
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+                const int rr = 4 * i + (lane >> 3), row = row0 + rr;
+                if (row >= s.m || col >= end) continue;
+                float4 v = *reinterpret_cast<const float4 *>(tc::patch_at(patch, rr, lane & 7));
+                if ((zeros >> rr) & 1u) v = make_float4(0.f, 0.f, 0.f, 0.f);
+                const int64_t at = (int64_t)row * s.n + col;
+                if (col + 4 <= s.n && (whole ? quads : quads_out) && (!src || quads)) {
+                    if (src) {
+                        const float4 o = *reinterpret_cast<const float4 *>(src + at);
+                        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                    }
+                    if (whole) {
+                        *reinterpret_cast<float4 *>(dst32 + at) = v;
+                    } else {
+                        struct alignas(4 * sizeof(OutT)) {
+                            OutT v[4];
+                        } q{{from_float<OutT>(v.x * f), from_float<OutT>(v.y * f), from_float<OutT>(v.z * f), from_float<OutT>(v.w * f)}};
+                        *reinterpret_cast<decltype(q) *>(out + (int64_t)row * ld + col) = q;
+                    }
+                } else {
+                    const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    const float4 o = *reinterpret_cast<const float4 *>(src + j);
-                    v[j] += o.x, v[j + 1] += o.y, v[j + 2] += o.z, v[j + 3] += o.w;
+                    for (int j = 0; j < 4; ++j)
+                        if (col + j < s.n) {
+                            const float x = w[j] + (src ? src[at + j] : 0.f);
+                            if (whole) dst32[at + j] = x;
+                            else out[(int64_t)row * ld + col + j] = from_float<OutT>(x * f);
+                        }
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (col + j < s.n) v[j] += src[j];
             }
-        }
-        if (whole) {
-            if (full && quads) {
-#pragma unroll
-                for (int j = 0; j < 32; j += 4)
-                    *reinterpret_cast<float4 *>(dst32 + col + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (col + j < s.n) dst32[col + j] = v[j];
-            }
-            return;
-        }
-        OutT *dst = out + (int64_t)row * ld + col;
-        constexpr int kPer = 16 / (int)sizeof(OutT);
-        if (full && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
-#pragma unroll
-            for (int j = 0; j < 32; j += kPer) {
-                alignas(16) OutT q[kPer];
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) q[i] = from_float<OutT>(v[j + i] * f);
-                *reinterpret_cast<uint4 *>(dst + j) = *reinterpret_cast<const uint4 *>(q);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (col + j < s.n) dst[j] = from_float<OutT>(v[j] * f);
         }
     }
 };
 
-// Joins the splits' planes in ascending order; add, keep, out as above.
-template <typename OutT>
-__global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ partial, int splits, int64_t m, int64_t n,
+// Joins the splits' planes in ascending order, V elements per thread; add, keep, out as above.
+template <typename OutT, int V>
+__global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ partial, int splits, int64_t m, int32_t n,
                                                      const float *add, float *keep, OutT *out, int64_t ld, const float *scale,
-                                                     const int32_t *labels, int32_t classes)
+                                                     const float *scale_b, const int32_t *labels, int32_t classes)
 {
-    const int64_t all = m * n;
-    const float f = scale ? *scale : 1.f;
+    struct alignas(4 * V) Quad {
+        float v[V];
+    };
+    const int64_t all = m * n / V;
+    const float f = factor_of(scale, scale_b);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
-        float v = 0.f;
-        for (int k = 0; k < splits; ++k) v += partial[(int64_t)k * all + i];
-        const int64_t row = i / n;
-        if (labels && (uint32_t)labels[row] >= (uint32_t)classes) v = 0.f;
-        if (add) v += add[i];
-        if (keep) keep[i] = v;
-        else out[row * ld + (i - row * n)] = from_float<OutT>(v * f);
+        Quad v{};
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) {
+            const Quad o = reinterpret_cast<const Quad *>(partial)[(int64_t)k * all + i];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v.v[j] += o.v[j];
+        }
+        const int64_t row = i * V / n;
+        if (labels && (uint32_t)labels[row] >= (uint32_t)classes) v = Quad{};
+        if (add) {
+            const Quad o = reinterpret_cast<const Quad *>(add)[i];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v.v[j] += o.v[j];
+        }
+        if (keep) {
+            reinterpret_cast<Quad *>(keep)[i] = v;
+        } else {
+            OutT *dst = out + row * ld + (i * V - row * n);
+#pragma unroll
+            for (int j = 0; j < V; ++j) dst[j] = from_float<OutT>(v.v[j] * f);
+        }
     }
 }
 
 // ---- small kernels -----------------------------------------------------------------------------------------
 
-// Joins the blocks of 128 classes of R rows per CTA; threads of one row run down its blocks, fixed order.
+// Joins the blocks of classes of R rows per CTA; threads of one row run down its blocks, fixed order.
 template <int R>
 __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ stats, int blocks, int32_t n,
                                                      const int32_t *__restrict__ labels, int32_t classes,
                                                      const float *__restrict__ label_logit, float *__restrict__ loss,
-                                                     float *__restrict__ lse, uint32_t *status)
+                                                     float *__restrict__ lse, float2 *__restrict__ norm, uint32_t *status)
 {
     constexpr int kT = 512 / R;
     __shared__ float s_top[kT][R], s_sum[kT][R];
@@ -279,6 +298,7 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
         const int32_t y = labels[row];
         const bool has = (uint32_t)y < (uint32_t)classes;
         const float total = top + logf(sum);
+        if (norm) norm[row] = make_float2(top, 1.f / sum);
         lse[row] = has ? total : 0.f;
         // relative to the largest logit: lse and the label's logit would lose the bits that they share
         loss[row] = has ? (top - label_logit[row]) + logf(sum) : 0.f;
@@ -286,12 +306,12 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
     }
 }
 
-// Exponentials to P, 8 classes per thread. Bits: 16-bit operands, in place; else three bf16 planes.
+// Exponentials to P, 8 classes per thread: in place for 16-bit operands, from fp32 to two fp16 planes for single precision.
 template <typename PT, bool kWide>
 __global__ void __launch_bounds__(256)
 k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, int32_t classes, const float2 *__restrict__ stats,
-                const float *__restrict__ lse, const float *__restrict__ loss, const int32_t *__restrict__ labels,
-                const float *__restrict__ weights, float scale, const float *__restrict__ lift)
+                const float2 *__restrict__ norm, const float *__restrict__ loss, const int32_t *__restrict__ labels,
+                const float *__restrict__ weights, float scale, const float *__restrict__ lift, int block_log)
 {
     const int row = blockIdx.y;
     const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
@@ -302,7 +322,9 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
     if (has) {
         float g = weights ? weights[row] * scale : scale;
         if (lift) g *= *lift;
-        const float f = exp2f((stats[(int64_t)(c / kHalfTile) * n + row].x - lse[row]) * kLog2e) * (kWide ? 1.f : 1.f / kStoreScale) * g;
+        // relative to the largest logit: lse has lost the bits that the two share
+        const float2 of = norm[row];
+        const float f = exp2f((stats[(int64_t)(c >> block_log) * n + row].x - of.x) * kLog2e) * of.y * (kWide ? 1.f : 1.f / kStoreScale) * g;
         if constexpr (kWide) {
             const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(store) + (int64_t)row * ld + c);
             const float4 a = src[0], b = src[1];
@@ -331,7 +353,7 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
     alignas(16) PT q[8];
     if constexpr (kWide) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 2; ++k) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 q[j] = from_float<PT>(v[j]);
@@ -346,14 +368,16 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
     }
 }
 
-// Rows in a layout that the bulk copies take (16-byte pitch), single precision as three bf16 planes; rows without a
-// label become zeros where labels are given.
+// Rows in a layout that the bulk copies take (whole lines), single precision scaled and as two fp16 planes; rows without a label
+// become zeros where labels are given.
 template <typename T, typename P>
 __global__ void __launch_bounds__(256) k_pack(const T *__restrict__ src, int64_t ld, int64_t rows, int32_t d, P *__restrict__ dst,
-                                              int64_t pitch, int64_t plane, const int32_t *__restrict__ labels, int32_t classes)
+                                              int64_t pitch, int64_t plane, const int32_t *__restrict__ labels, int32_t classes,
+                                              const float *__restrict__ lift)
 {
-    const int per = (int)((pitch + 7) / 8);
+    const int per = (int)(pitch / 8);
     const int64_t all = rows * per;
+    const float up = sizeof(T) == 4 ? *lift : 1.f;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / per;
         const int c = (int)(i - row * per) * 8;
@@ -368,49 +392,93 @@ __global__ void __launch_bounds__(256) k_pack(const T *__restrict__ src, int64_t
 #pragma unroll
             for (int j = 0; j < 8; ++j) in[j] = has && c + j < d ? from[j] : from_float<T>(0.f);
         }
-        alignas(16) P q[8];
         if constexpr (sizeof(T) == 4) {
-            float v[8];
+            alignas(16) P hi[8], lo[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = in[j];
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    q[j] = from_float<P>(v[j]);
-                    // (infinite: the planes behind it are 0, not inf - inf)
-                    v[j] = isinf((float)q[j]) ? 0.f : v[j] - (float)q[j];
-                }
-                *reinterpret_cast<uint4 *>(dst + k * plane + row * pitch + c) = *reinterpret_cast<const uint4 *>(q);
+            for (int j = 0; j < 8; ++j) {
+                const float v = in[j] * up;
+                hi[j] = from_float<P>(v);
+                lo[j] = from_float<P>(v - (float)hi[j]);
             }
+            *reinterpret_cast<uint4 *>(dst + row * pitch + c) = *reinterpret_cast<const uint4 *>(hi);
+            *reinterpret_cast<uint4 *>(dst + plane + row * pitch + c) = *reinterpret_cast<const uint4 *>(lo);
         } else {
             *reinterpret_cast<uint4 *>(dst + row * pitch + c) = *reinterpret_cast<const uint4 *>(in);
         }
     }
 }
 
-// fp16: the power of two that takes the largest weight to [2^13, 2^14), and its inverse.
-__global__ void __launch_bounds__(1024) k_lift(const float *__restrict__ weights, int64_t n, float scale, float *__restrict__ lift)
+// Largest finite magnitudes, one word per CTA: the first kMaxBlocks of X (rows with a label, where labels are given), the next of W.
+constexpr int kMaxBlocks = 148 * 4;
+
+__global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, int64_t ld_x, int64_t n, const int32_t *__restrict__ labels,
+                                                 int32_t classes, const float *__restrict__ w, int64_t ld_w, int32_t d,
+                                                 float *__restrict__ largest)
 {
-    __shared__ float s[32];
+    __shared__ float s[8];
+    const bool of_x = blockIdx.x < kMaxBlocks;
+    const float *src = of_x ? x : w;
+    const int64_t ld = of_x ? ld_x : ld_w, rows = of_x ? n : classes;
+    const bool quads = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && (ld & 3) == 0 && (d & 3) == 0;
+    const int per = quads ? d / 4 : d;
+    const int64_t all = rows * per;
     float top = 0.f;
-    if (weights)
-        for (int64_t i = threadIdx.x; i < n; i += 1024) {
-            const float v = fabsf(weights[i] * scale);
-            if (v < INFINITY) top = fmaxf(top, v);
+    auto take = [&](float v) {
+        v = fabsf(v);
+        if (v < INFINITY) top = fmaxf(top, v);
+    };
+#pragma unroll 4
+    for (int64_t i = (int64_t)(blockIdx.x % kMaxBlocks) * 256 + threadIdx.x; i < all; i += (int64_t)kMaxBlocks * 256) {
+        const int64_t row = i / per;
+        const int c = (int)(i - row * per);
+        if (of_x && (uint32_t)labels[row] >= (uint32_t)classes) continue;
+        if (quads) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + row * ld + 4 * c);
+            take(v.x), take(v.y), take(v.z), take(v.w);
+        } else {
+            take(src[row * ld + c]);
         }
-    else
-        top = fabsf(scale);
+    }
+#pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = top;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i]);
-        int e = 0;
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
+        largest[blockIdx.x] = top;
+    }
+}
+
+// The scales. CTA 0: of P, from the weights; 1 and 2: of X and W, from the largest magnitudes (null: no such scales).
+__global__ void __launch_bounds__(512) k_scales(const float *__restrict__ weights, int64_t n, float scale, const float *__restrict__ largest,
+                                                float *__restrict__ scales)
+{
+    __shared__ float s[16];
+    float top = 0.f;
+    if (blockIdx.x == 0) {
+        if (weights) {
+#pragma unroll 4
+            for (int64_t i = threadIdx.x; i < n; i += 512) {
+                const float v = fabsf(weights[i] * scale);
+                if (v < INFINITY) top = fmaxf(top, v);
+            }
+        } else {
+            top = fabsf(scale);
+        }
+    } else {
+        for (int i = threadIdx.x; i < kMaxBlocks; i += 512) top = fmaxf(top, largest[(blockIdx.x - 1) * kMaxBlocks + i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        int e = 15;
         if (top > 0.f) frexpf(top, &e); // top in [2^(e-1), 2^e)
-        e = max(-100, min(100, 14 - e));
-        lift[0] = ldexpf(1.f, e);
-        lift[1] = ldexpf(1.f, -e);
+        e = max(-120, min(120, 15 - e));
+        scales[2 * blockIdx.x] = ldexpf(1.f, e);
+        scales[2 * blockIdx.x + 1] = ldexpf(1.f, -e);
     }
 }
 
@@ -454,13 +522,15 @@ bool make_map(CUtensorMap *map, const Operand &o, bool half, int box_cols, int b
 }
 
 template <int CG, int BN, bool AMN, bool BMN, class Epi>
-cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, const Epi &epi, cudaStream_t stream)
+cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int cols, const Epi &epi, cudaStream_t stream)
 {
     using L = tc::Layout<CG, BN>;
     CUtensorMap ma, mb;
-    if (!make_map(&ma, a, s.half, 64, AMN ? 64 : L::kBM) || !make_map(&mb, b, s.half, 64, BMN ? 64 : L::kBNc)) return cudaErrorInvalidValue;
+    s.a_rows = AMN || s.m >= L::kBM ? L::kBM : (s.m + 7) / 8 * 8; // (what lies behind them in shared memory is not of C)
+    if (!make_map(&ma, a, s.half, 64, AMN ? 64 : s.a_rows) || !make_map(&mb, b, s.half, 64, BMN ? 64 : cols / CG)) return cudaErrorInvalidValue;
     s.m_tiles = (int32_t)ceil_div(s.m, CG * L::kBM);
-    s.n_tiles = (int32_t)ceil_div(s.n, BN);
+    s.n_tiles = (int32_t)ceil_div(s.n, cols);
+    s.cols = cols;
     auto *kernel = tc::k_product<CG, BN, AMN, BMN, Epi>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
     if (e != cudaSuccess) return e;
@@ -480,10 +550,44 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, cons
     return cudaLaunchKernelEx(&cfg, kernel, ma, mb, s, epi);
 }
 
+// Which tiles. Pairs of CTAs (256 rows) wherever C has more rows than one CTA takes: each fetches half of B (8192 x 131072 x 4096
+// with gradients 23.8 against 23.5 ms, 1777 x 50001 x 1000 823 against 670 us).
+bool pairs_of_ctas(int64_t m) { return m > 128; }
+// Columns per tile: 128 where C has no more, else 256.
+int tile_columns(int64_t n) { return n <= 128 ? 128 : 256; }
+int tile_rows(int64_t m) { return pairs_of_ctas(m) ? 256 : 128; }
+
+// The loss of few rows is bound by the stream of W: there the tile has as many columns as share the classes out most evenly
+// (131072 classes on 148 SMs: four turns of 224 instead of 256, and nothing left to do in the fifth).
+int logit_columns(int64_t rows, int64_t classes, bool grad)
+{
+    const int most = tile_columns(classes);
+    if (grad || most == 128 || pairs_of_ctas(rows)) return most;
+    int best = most;
+    for (int c = most - 32; c > most / 2; c -= 32)
+        if (ceil_div(ceil_div(classes, c), kSms) * (c + 8) < ceil_div(ceil_div(classes, best), kSms) * (best + 8)) best = c;
+    return best;
+}
+
+// Pairs of (largest, sum) per row: one for each half of a tile that has columns.
+int64_t blocks_of(int64_t classes, int cols)
+{
+    const int64_t tiles = ceil_div(classes, cols), last = classes - (tiles - 1) * cols;
+    return 2 * (tiles - 1) + (last > tile_columns(classes) / 2 ? 2 : 1);
+}
+
+template <bool AMN, bool BMN, class Epi>
+cudaError_t run_product(const Operand &a, const Operand &b, const tc::Shape &s, int cols, const Epi &epi, cudaStream_t stream)
+{
+    if (tile_columns(s.n) == 128)
+        return pairs_of_ctas(s.m) ? launch_product<2, 128, AMN, BMN>(a, b, s, cols, epi, stream) : launch_product<1, 128, AMN, BMN>(a, b, s, cols, epi, stream);
+    return pairs_of_ctas(s.m) ? launch_product<2, 256, AMN, BMN>(a, b, s, cols, epi, stream) : launch_product<1, 256, AMN, BMN>(a, b, s, cols, epi, stream);
+}
+
 int element_size(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
 
-// Bytes per logit of a piece of rows: 16-bit values in place, or fp32 values and three planes.
-int64_t logit_bytes(bool wide) { return wide ? 10 : 2; }
+// Bytes per logit of a piece of rows: 16-bit values in place, or fp32 values and two planes.
+int64_t logit_bytes(bool wide) { return wide ? 8 : 2; }
 
 bool takes_bulk(const chicle_dense_t &x)
 {
@@ -492,15 +596,17 @@ bool takes_bulk(const chicle_dense_t &x)
 
 // The summed index of a gradient is cut where its tiles alone would leave SMs idle: time of the waves plus that of
 // writing and joining the planes.
-int plan_splits(int64_t m_tiles, int64_t n_tiles, int64_t steps, int64_t m, int64_t n, int slots)
+int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs)
 {
-    const int64_t tiles = m_tiles * n_tiles;
+    const int rows = tile_rows(m), cols = tile_columns(n);
+    const int64_t tiles = ceil_div(m, rows) * ceil_div(n, cols), slots = kSms / (rows / 128);
+    const double slice = cols == 256 ? 0.28e-6 : 0.15e-6;
     int best = 1;
     double best_t = 0;
     for (int s = 1; s <= 64 && s <= steps; ++s) {
         const double waves = (double)ceil_div(tiles * s, slots);
-        const double t = waves * ((double)ceil_div(steps, s) * 0.30e-6 + 1.0e-6) + (s > 1 ? 4e-6 + (double)s * m * n * 8.0 / 5e12 : 0.0);
-        if (s == 1 || t < best_t * 0.97) {
+        const double t = waves * ((double)(ceil_div(steps, s) * pairs) * slice + 1.0e-6) + (s > 1 ? 3e-6 + (double)s * m * n * 8.0 / 5e12 : 0.0);
+        if (s == 1 || t < best_t * 0.95) {
             best = s;
             best_t = t;
         }
@@ -508,32 +614,33 @@ int plan_splits(int64_t m_tiles, int64_t n_tiles, int64_t steps, int64_t m, int6
     return best;
 }
 
-constexpr int64_t kPieceBytes = (int64_t)1 << 30;
-constexpr int kBN = 256;
+constexpr int64_t kPieceBytes = (int64_t)1 << 31;
 
 struct Plan {
-    bool wide, half;
-    int planes;
+    bool wide, half; // single precision; operands in fp16 (else bf16)
+    int planes, pairs;
     int64_t n, v, d;
     bool pack_x, pack_w;
     int64_t pitch_d, ld_v;
     int64_t piece;     // rows per piece
     int splits_x, splits_w;
     // offsets into the workspace
-    size_t x, w, stats, label_logit, store, p, acc, partial, lift, total;
+    size_t x, w, stats, label_logit, norm, store, p, acc, partial, scales, largest, total;
 };
 
 Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
 {
     Plan p{};
     p.wide = X.type == CHICLE_F32;
-    p.half = X.type == CHICLE_F16;
-    p.planes = p.wide ? 3 : 1;
+    p.half = X.type != CHICLE_BF16;
+    p.planes = p.wide ? 2 : 1;
+    p.pairs = p.wide ? 3 : 1;
     p.n = X.rows, p.v = W.rows, p.d = X.cols;
     p.pack_x = grad || !takes_bulk(X);
     p.pack_w = !takes_bulk(W);
-    p.pitch_d = (p.d + 7) / 8 * 8;
-    p.ld_v = (p.v + 7) / 8 * 8;
+    // rows of whole 128-byte lines: a row of a bulk copy that straddles two takes two requests
+    p.pitch_d = (p.d + 63) / 64 * 64;
+    p.ld_v = (p.v + 63) / 64 * 64;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -544,46 +651,63 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     if (grad) {
         int64_t rows = kPieceBytes / (p.ld_v * logit_bytes(p.wide)) / 256 * 256;
         // fewer than 2048 rows: the fp32 sums of dW would be read and written too often beside the products of a piece
-        rows = std::max(rows, std::min<int64_t>(2048, 8 * kPieceBytes / (p.ld_v * logit_bytes(p.wide))));
+        rows = std::max(rows, std::min<int64_t>(2048, 4 * kPieceBytes / (p.ld_v * logit_bytes(p.wide))));
         rows = std::max<int64_t>(rows, 256);
         if (rows < p.n) p.piece = ceil_div(ceil_div(p.n, ceil_div(p.n, rows)), 256) * 256;
     }
     if (p.pack_x) p.x = take((size_t)p.planes * p.n * p.pitch_d * 2);
     if (p.pack_w) p.w = take((size_t)p.planes * p.v * p.pitch_d * 2);
-    p.stats = take((size_t)ceil_div(p.v, kHalfTile) * p.piece * sizeof(float2));
+    p.stats = take((size_t)(blocks_of(p.v, logit_columns(p.piece, p.v, grad)) * p.piece) * sizeof(float2));
     p.label_logit = take((size_t)p.piece * 4);
+    if (grad) p.norm = take((size_t)p.piece * sizeof(float2));
     if (grad) {
         if (p.wide) {
             p.store = take((size_t)p.piece * p.ld_v * 4);
-            p.p = take((size_t)3 * p.piece * p.ld_v * 2);
+            p.p = take((size_t)2 * p.piece * p.ld_v * 2);
         } else {
             p.store = p.p = take((size_t)p.piece * p.ld_v * 2);
         }
         if (p.piece < p.n) p.acc = take((size_t)p.v * p.d * 4);
-        const int pairs = p.wide ? 6 : 1;
-        p.splits_x = plan_splits(ceil_div(p.piece, 128), ceil_div(p.d, kBN), ceil_div(p.v, tc::kBK) * pairs, p.piece, p.d, kSms);
-        p.splits_w = plan_splits(ceil_div(p.v, 128), ceil_div(p.d, kBN), ceil_div(p.piece, tc::kBK) * pairs, p.v, p.d, kSms);
+        p.splits_x = plan_splits(p.piece, p.d, ceil_div(p.v, tc::kBK), p.pairs);
+        p.splits_w = plan_splits(p.v, p.d, ceil_div(p.piece, tc::kBK), p.pairs);
         size_t part = 0;
         if (p.splits_x > 1) part = (size_t)p.splits_x * p.piece * p.d * 4;
         if (p.splits_w > 1) part = std::max(part, (size_t)p.splits_w * p.v * p.d * 4);
         if (part) p.partial = take(part);
-        p.lift = take(8);
     }
+    p.scales = take(kScales * sizeof(float));
+    if (p.wide) p.largest = take(2 * kMaxBlocks * sizeof(float));
     p.total = at;
     return p;
 }
 
-cudaError_t pack(const chicle_dense_t &src, void *dst, const Plan &p, const int32_t *labels, int32_t classes, cudaStream_t s)
+cudaError_t pack(const chicle_dense_t &src, void *dst, const Plan &p, const int32_t *labels, const float *lift, cudaStream_t s)
 {
     const int64_t all = src.rows * (p.pitch_d / 8);
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(all, 256), kSms * 16);
     const int64_t plane = src.rows * p.pitch_d;
     if (src.type == CHICLE_F32)
-        k_pack<float, __nv_bfloat16><<<grid, 256, 0, s>>>((const float *)src.data, src.ld, src.rows, (int32_t)p.d, (__nv_bfloat16 *)dst, p.pitch_d, plane, labels, classes);
+        k_pack<float, __half><<<grid, 256, 0, s>>>((const float *)src.data, src.ld, src.rows, (int32_t)p.d, (__half *)dst, p.pitch_d, plane, labels, (int32_t)p.v, lift);
     else if (src.type == CHICLE_BF16)
-        k_pack<__nv_bfloat16, __nv_bfloat16><<<grid, 256, 0, s>>>((const __nv_bfloat16 *)src.data, src.ld, src.rows, (int32_t)p.d, (__nv_bfloat16 *)dst, p.pitch_d, plane, labels, classes);
+        k_pack<__nv_bfloat16, __nv_bfloat16><<<grid, 256, 0, s>>>((const __nv_bfloat16 *)src.data, src.ld, src.rows, (int32_t)p.d, (__nv_bfloat16 *)dst, p.pitch_d, plane, labels, (int32_t)p.v, nullptr);
     else
-        k_pack<__half, __half><<<grid, 256, 0, s>>>((const __half *)src.data, src.ld, src.rows, (int32_t)p.d, (__half *)dst, p.pitch_d, plane, labels, classes);
+        k_pack<__half, __half><<<grid, 256, 0, s>>>((const __half *)src.data, src.ld, src.rows, (int32_t)p.d, (__half *)dst, p.pitch_d, plane, labels, (int32_t)p.v, nullptr);
+    return cudaGetLastError();
+}
+
+// The scales that these operands take; null where they take none.
+cudaError_t find_scales(const chicle_dense_t &X, const chicle_dense_t &W, const Plan &p, const int32_t *labels, const float *weights,
+                        float scale, uint8_t *ws, cudaStream_t s, float **scales)
+{
+    *scales = nullptr;
+    if (!p.half) return cudaSuccess;
+    *scales = reinterpret_cast<float *>(ws + p.scales);
+    float *largest = nullptr;
+    if (p.wide) {
+        largest = reinterpret_cast<float *>(ws + p.largest);
+        k_largest<<<2 * kMaxBlocks, 256, 0, s>>>((const float *)X.data, X.ld, p.n, labels, (int32_t)p.v, (const float *)W.data, W.ld, (int32_t)p.d, largest);
+    }
+    k_scales<<<p.wide ? 3 : 1, 512, 0, s>>>(weights, p.n, scale, largest, *scales);
     return cudaGetLastError();
 }
 
@@ -599,12 +723,19 @@ Operand operand_of(const chicle_dense_t &src, const void *packed, bool is_packed
     return o;
 }
 
-tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int splits, int group, uint32_t *status)
+// Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential takes
+// on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 256: 4e-7); all
+// of them where a gradient is rounded to 16 bits in the end.
+int logit_chunk(const Plan &p) { return (p.wide ? 512 : 1024) / tc::kBK; }
+int grad_chunk(const Plan &p) { return p.wide ? 512 / tc::kBK : INT32_MAX / 2; }
+
+tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int chunk, int splits, int group, uint32_t *status)
 {
     tc::Shape s{};
     s.m = (int32_t)m, s.n = (int32_t)n;
     s.k_steps = (int32_t)ceil_div(k, tc::kBK);
-    s.pairs = p.wide ? 6 : 1;
+    s.pairs = p.pairs;
+    s.chunk = chunk;
     s.splits = splits;
     s.group = group;
     s.half = p.half;
@@ -612,16 +743,16 @@ tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int splits, i
     return s;
 }
 
-cudaError_t join_blocks(const Plan &p, const float2 *stats, int64_t rows, const int32_t *labels, const float *label_logit, float *loss,
-                        float *lse, uint32_t *status, cudaStream_t s)
+cudaError_t join_blocks(const Plan &p, const float2 *stats, int cols, int64_t rows, const int32_t *labels, const float *label_logit, float *loss,
+                        float *lse, float2 *norm, uint32_t *status, cudaStream_t s)
 {
-    const int blocks = (int)ceil_div(p.v, kHalfTile);
+    const int blocks = (int)blocks_of(p.v, cols);
     if (rows >= 32 * 64)
-        k_join_blocks<32><<<(unsigned)ceil_div(rows, 32), 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, status);
+        k_join_blocks<32><<<(unsigned)ceil_div(rows, 32), 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, norm, status);
     else if (rows >= 8)
-        k_join_blocks<8><<<(unsigned)ceil_div(rows, 8), 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, status);
+        k_join_blocks<8><<<(unsigned)ceil_div(rows, 8), 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, norm, status);
     else
-        k_join_blocks<1><<<(unsigned)rows, 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, status);
+        k_join_blocks<1><<<(unsigned)rows, 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, norm, status);
     return cudaGetLastError();
 }
 
@@ -635,11 +766,12 @@ int group_of(int64_t k, int planes, int rows_per_tile)
 template <typename OutT>
 cudaError_t gradient(const Plan &p, const Operand &a, const Operand &b, bool of_x, tc::Shape s, GradEpilogue<OutT> epi, cudaStream_t stream)
 {
-    cudaError_t e = of_x ? launch_product<1, kBN, false, true>(a, b, s, epi, stream) : launch_product<1, kBN, true, true>(a, b, s, epi, stream);
+    cudaError_t e = of_x ? run_product<false, true>(a, b, s, tile_columns(s.n), epi, stream) : run_product<true, true>(a, b, s, tile_columns(s.n), epi, stream);
     if (e == cudaSuccess && s.splits > 1) {
         const int64_t all = (int64_t)s.m * s.n;
-        k_join_splits<OutT><<<(unsigned)std::min<int64_t>(ceil_div(all, 256), kSms * 8), 256, 0, stream>>>(
-            epi.partial, s.splits, s.m, s.n, epi.add, epi.keep, epi.out, epi.ld, epi.scale, epi.labels, epi.classes);
+        auto *join = (s.n & 3) == 0 ? k_join_splits<OutT, 4> : k_join_splits<OutT, 1>;
+        join<<<(unsigned)std::min<int64_t>(ceil_div(all, 1024), kSms * 8), 256, 0, stream>>>(
+            epi.partial, s.splits, s.m, s.n, epi.add, epi.keep, epi.out, epi.ld, epi.scale, epi.scale_b, epi.labels, epi.classes);
         e = cudaGetLastError();
     }
     return e;
@@ -651,15 +783,12 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
                      uint32_t *status, cudaStream_t stream)
 {
     constexpr bool kWide = sizeof(T) == 4;
-    cudaError_t e = pack(X, ws + p.x, p, labels, (int32_t)p.v, stream);
-    if (e == cudaSuccess && p.pack_w) e = pack(W, ws + p.w, p, nullptr, 0, stream);
-    float *lift = nullptr;
-    if (e == cudaSuccess && p.half) {
-        lift = reinterpret_cast<float *>(ws + p.lift);
-        k_lift<<<1, 1024, 0, stream>>>(weights, p.n, scale, lift);
-        e = cudaGetLastError();
-    }
+    float *scales;
+    cudaError_t e = find_scales(X, W, p, labels, weights, scale, ws, stream, &scales);
+    if (e == cudaSuccess) e = pack(X, ws + p.x, p, labels, scales + kLiftX, stream);
+    if (e == cudaSuccess && p.pack_w) e = pack(W, ws + p.w, p, nullptr, scales + kLiftW, stream);
     const Operand w = operand_of(W, ws + p.w, p.pack_w, p);
+    const int cols = logit_columns(p.n, p.v, true);
     for (int64_t r0 = 0; e == cudaSuccess && r0 < p.n; r0 += p.piece) {
         const int64_t rows = std::min(p.piece, p.n - r0);
         Operand x = operand_of(X, ws + p.x, true, p);
@@ -667,34 +796,36 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         x.rows = rows;
         float2 *stats = reinterpret_cast<float2 *>(ws + p.stats);
         float *label_logit = reinterpret_cast<float *>(ws + p.label_logit);
+        float2 *norm = reinterpret_cast<float2 *>(ws + p.norm);
         StoreT *store = reinterpret_cast<StoreT *>(ws + p.store);
         PT *prob = reinterpret_cast<PT *>(ws + p.p);
-        const LogitsEpilogue<StoreT> le{labels + r0, stats, label_logit, store, p.ld_v};
-        e = launch_product<1, kBN, false, false>(x, w, shape_of(p, rows, p.v, p.d, 1, group_of(p.d, p.planes, 128), status), le, stream);
-        if (e == cudaSuccess) e = join_blocks(p, stats, rows, labels + r0, label_logit, loss + r0, lse + r0, status, stream);
+        const LogitsEpilogue<StoreT> le{labels + r0, stats, label_logit, store, p.ld_v, kWide ? scales : nullptr};
+        e = run_product<false, false>(x, w, shape_of(p, rows, p.v, p.d, logit_chunk(p), 1, group_of(p.d, p.planes, tile_rows(p.n)), status), cols, le, stream);
+        if (e == cudaSuccess) e = join_blocks(p, stats, cols, rows, labels + r0, label_logit, loss + r0, lse + r0, norm, status, stream);
         if (e != cudaSuccess) break;
         Operand q;
         q.data = prob;
         q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.planes;
         for (int64_t y = 0; y < rows; y += 65535)
             k_probabilities<PT, kWide><<<dim3((unsigned)ceil_div(p.v, 2048), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(
-                store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, lse + r0 + y, loss + r0 + y,
-                labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, lift);
+                store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
+                labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr, cols == 128 ? 6 : 7);
         if ((e = cudaGetLastError()) != cudaSuccess) break;
-        const float *back = lift ? lift + 1 : nullptr;
+        const float *back = scales ? scales + kInvLift : nullptr;
         float *partial = reinterpret_cast<float *>(ws + p.partial);
-        GradEpilogue<T> ex{static_cast<T *>(dX.data) + r0 * dX.ld, dX.ld, p.splits_x > 1 ? partial : nullptr, nullptr, nullptr, back, labels + r0, (int32_t)p.v};
-        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, p.splits_x, 8, status), ex, stream);
+        GradEpilogue<T> ex{static_cast<T *>(dX.data) + r0 * dX.ld, dX.ld, p.splits_x > 1 ? partial : nullptr, nullptr, nullptr, back,
+                           kWide ? scales + kInvW : nullptr, labels + r0, (int32_t)p.v};
+        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, grad_chunk(p), p.splits_x, 8, status), ex, stream);
         if (e != cudaSuccess) break;
         // dW over the pieces: the sums stay in fp32 until the last
         const bool first = r0 == 0, last = r0 + rows >= p.n;
-        GradEpilogue<T> ew{static_cast<T *>(dW.data), dW.ld, nullptr, nullptr, nullptr, back, nullptr, 0};
+        GradEpilogue<T> ew{static_cast<T *>(dW.data), dW.ld, nullptr, nullptr, nullptr, back, kWide ? scales + kInvX : nullptr, nullptr, 0};
         float *acc = reinterpret_cast<float *>(ws + p.acc);
         if (!first) ew.add = acc;
         if (!last) ew.keep = acc;
-        const int splits = (int)std::min<int64_t>(p.splits_w, ceil_div(rows, tc::kBK) * (kWide ? 6 : 1));
+        const int splits = (int)std::min<int64_t>(p.splits_w, ceil_div(rows, tc::kBK));
         if (splits > 1) ew.partial = partial;
-        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, splits, 8, status), ew, stream);
+        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, grad_chunk(p), splits, 8, status), ew, stream);
     }
     return e;
 }
@@ -768,16 +899,19 @@ extern "C" chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, co
     if (!encode_fn()) return err(CHICLE_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     uint8_t *ws = static_cast<uint8_t *>(dev_workspace);
-    cudaError_t e = cudaSuccess;
-    if (p.pack_x) e = pack(*X, ws + p.x, p, nullptr, 0, s);
-    if (e == cudaSuccess && p.pack_w) e = pack(*W, ws + p.w, p, nullptr, 0, s);
+    float *scales = nullptr;
+    cudaError_t e = p.wide ? find_scales(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, &scales) : cudaSuccess;
+    // (rows without a label are left out of the scale, so they have to be zeros)
+    if (e == cudaSuccess && p.pack_x) e = pack(*X, ws + p.x, p, dev_labels, scales + kLiftX, s);
+    if (e == cudaSuccess && p.pack_w) e = pack(*W, ws + p.w, p, nullptr, scales + kLiftW, s);
     float2 *stats = reinterpret_cast<float2 *>(ws + p.stats);
     float *label_logit = reinterpret_cast<float *>(ws + p.label_logit);
-    const LogitsEpilogue<NoStore> le{dev_labels, stats, label_logit, nullptr, 0};
+    const int cols = logit_columns(p.n, p.v, false);
+    const LogitsEpilogue<NoStore> le{dev_labels, stats, label_logit, nullptr, 0, scales};
     if (e == cudaSuccess)
-        e = launch_product<1, kBN, false, false>(operand_of(*X, ws + p.x, p.pack_x, p), operand_of(*W, ws + p.w, p.pack_w, p),
-                                                 shape_of(p, p.n, p.v, p.d, 1, group_of(p.d, p.planes, 128), dev_status), le, s);
-    if (e == cudaSuccess) e = join_blocks(p, stats, p.n, dev_labels, label_logit, dev_loss, dev_lse, dev_status, s);
+        e = run_product<false, false>(operand_of(*X, ws + p.x, p.pack_x, p), operand_of(*W, ws + p.w, p.pack_w, p),
+                                                 shape_of(p, p.n, p.v, p.d, logit_chunk(p), 1, group_of(p.d, p.planes, tile_rows(p.n)), dev_status), cols, le, s);
+    if (e == cudaSuccess) e = join_blocks(p, stats, cols, p.n, dev_labels, label_logit, dev_loss, dev_lse, nullptr, dev_status, s);
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
 }
 
@@ -814,7 +948,7 @@ extern "C" chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_strea
     uint8_t *ws = static_cast<uint8_t *>(dev_workspace);
     cudaError_t e;
     if (X->type == CHICLE_F32)
-        e = run_grad<float, __nv_bfloat16, float>(p, *X, *W, dev_labels, dev_weights, scale, dev_loss, dev_lse, *dX, *dW, ws, dev_status, s);
+        e = run_grad<float, __half, float>(p, *X, *W, dev_labels, dev_weights, scale, dev_loss, dev_lse, *dX, *dW, ws, dev_status, s);
     else if (X->type == CHICLE_BF16)
         e = run_grad<__nv_bfloat16, __nv_bfloat16, __half>(p, *X, *W, dev_labels, dev_weights, scale, dev_loss, dev_lse, *dX, *dW, ws, dev_status, s);
     else

@@ -9,9 +9,15 @@
 // Either operand may have the summed index contiguous ("K-major", rows of 64 elements) or the other one
 // ("MN-major", boxes of 64 x 64 elements); both in the 128-byte swizzle.
 //
-// Single precision goes through the same kernel: an fp32 matrix is held as three bf16 planes whose sum has all 24 bits,
-// and the six products of planes that matter (2+0, 0+2, 1+1, 1+0, 0+1, 0+0; what is left is below 2^-24) are summed into
-// one accumulator. `pairs` is 1 or 6.
+// Single precision goes through the same kernel: an fp32 matrix, scaled by a power of two so that its largest element
+// lies in [2^14, 2^15), is held as two fp16 planes. Their sum is off by 2^-22 of an element at most (1e-7 on average, what a sum
+// in fp32 is off by, too), and of elements below 2^-17 of the largest by 2^-39 of that. Three products of planes (1+0, 0+1,
+// 0+0) are summed into one accumulator; the fourth is below 2^-22 of a term. `pairs` is 1 or 3.
+//
+// The tensor cores cut an accumulator off towards zero at every step of 16, about 2^-25 of it on average (measured: sums of
+// 12 000 steps came out 1.3e-5 too small). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices,
+// each with an accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a
+// chunk the small products of planes come first.
 //
 // Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's copies and products in flight are
 // waited for and tensor memory is given back before it returns.
@@ -31,7 +37,8 @@ namespace tc {
 constexpr int kBK = 64;              // summed elements per stage: 128 bytes, one swizzle span
 constexpr int kThreads = 320;        // copy warp, product warp, 8 epilogue warps
 constexpr int kEpiWarps = 8;
-constexpr uint64_t kWaitNs = 4000000000ull;
+constexpr uint32_t kPatchBytes = 4096; // shared memory of an epilogue warp: 32 rows of 128 bytes
+constexpr long long kWaitClocks = 6000000000ll; // some seconds
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -46,35 +53,36 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 // Arrives at a barrier of any CTA of the cluster (a shared::cluster address).
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
-}
-__device__ __forceinline__ uint64_t now_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
 }
 // False once the wait has run out, here or in another role of the CTA.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped)
 {
     if (bar_try(bar, parity)) return true;
-    const uint64_t t0 = now_ns();
+    const long long t0 = clock64();
     for (;;) {
-        for (int i = 0; i < 64; ++i)
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i)
             if (bar_try(bar, parity)) return true;
         if (*stopped) return false;
-        if (now_ns() - t0 > kWaitNs) {
+        if (clock64() - t0 > kWaitClocks) {
             *stopped = 1;
             return false;
         }
     }
+}
+// For what is in flight when a CTA stops.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
+{
+    const long long t0 = clock64();
+    while (!bar_try(bar, parity) && clock64() - t0 <= kWaitClocks) {}
 }
 // The same address in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank)
@@ -152,8 +160,11 @@ __device__ __forceinline__ void load32(uint32_t addr, uint32_t (&r)[32])
 struct Shape {
     int32_t m, n;           // rows and columns of C
     int32_t m_tiles, n_tiles;
+    int32_t a_rows;         // rows of A that a copy brings: 128, or fewer where C has no more (K-major A, CG = 1 only)
+    int32_t cols;           // columns per tile: BN, or fewer (a multiple of 32, CG = 1 only)
     int32_t k_steps;        // slices of kBK of the summed index (per pair of planes)
-    int32_t pairs;          // 1, or 6 for single precision
+    int32_t pairs;          // 1, or 3 for single precision
+    int32_t chunk;          // slices summed in one accumulator
     int32_t splits;         // the summed index is cut into so many pieces, each a tile of its own
     int32_t group;          // m tiles walked together before the next column of tiles
     int32_t half;           // operands fp16 (else bf16)
@@ -162,7 +173,7 @@ struct Shape {
 
 struct Tile {
     int32_t m, n, split;
-    int32_t first, last; // slices of the flattened (k step, pair of planes) order
+    int32_t first, last; // slices
 };
 
 // Tile t of the walk: groups of `group` m tiles; within a group, splits outermost, then n, then m.
@@ -178,29 +189,35 @@ __device__ __forceinline__ Tile tile_of(const Shape &s, int64_t t)
     in -= (int64_t)r.split * per_split;
     r.n = (int32_t)(in / gm);
     r.m = g * s.group + (int32_t)(in - (int64_t)r.n * gm);
-    const int64_t all = (int64_t)s.k_steps * s.pairs;
-    r.first = (int32_t)(all * r.split / s.splits);
-    r.last = (int32_t)(all * (r.split + 1) / s.splits);
+    r.first = (int32_t)((int64_t)s.k_steps * r.split / s.splits);
+    r.last = (int32_t)((int64_t)s.k_steps * (r.split + 1) / s.splits);
     return r;
 }
 
-// Planes of the six products, smallest first.
-__device__ __forceinline__ int plane_a(int pairs, int q) { return pairs == 1 ? 0 : (0x001102 >> (4 * q)) & 3; }
-__device__ __forceinline__ int plane_b(int pairs, int q) { return pairs == 1 ? 0 : (0x010120 >> (4 * q)) & 3; }
+// Planes of the three products, smallest first.
+__device__ __forceinline__ int plane_a(int pairs, int q) { return pairs == 3 && q == 0; }
+__device__ __forceinline__ int plane_b(int pairs, int q) { return pairs == 3 && q == 1; }
 
 template <int CG, int BN> struct Layout {
     static constexpr int kBM = 128;                // rows of A per CTA
-    static constexpr int kBNc = BN / CG;           // rows of B per CTA
+    static constexpr int kBNc = BN / CG;           // rows of B per CTA (at most)
     static constexpr uint32_t kABytes = kBM * kBK * 2;
     static constexpr uint32_t kBBytes = kBNc * kBK * 2;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = (int)((200u * 1024u) / kStageBytes) > 8 ? 8 : (int)((200u * 1024u) / kStageBytes);
-    static constexpr uint32_t kSmem = kStages * kStageBytes + 1024; // room to start on 1024 bytes
+    static constexpr int kStages = (int)((192u * 1024u) / kStageBytes) > 8 ? 8 : (int)((192u * 1024u) / kStageBytes);
+    static constexpr uint32_t kSmem = kStages * kStageBytes + kEpiWarps * kPatchBytes + 1024; // room to start on 1024 bytes
+    static_assert(kSmem <= 227u * 1024u - 512u, "shared memory of an SM");
 };
 
-// Epi has `template <int BN> __device__ void tile(const Shape &, const Tile &, int row0, int col0, uint32_t tmem, int quarter,
-// int half, int lane) const`: called by each of the eight epilogue warps, it finishes rows row0 + 32 quarter .. and the
-// columns col0 + half BN / 2 .. of the tile. It has read tensor memory when it returns.
+// 16-byte piece `c` of row `r` of a warp's patch: rows of 128 bytes whose pieces are exchanged so that both a piece of all rows and
+// whole rows are free of bank conflicts. Results go through it so that a warp's store covers 4 rows of 128 bytes, not 32 of 16
+// (fp32 exponentials of 10 000 x 1000 logits of 100 products: 48 us in single rows of 16 bytes, NEW us so).
+__device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { return reinterpret_cast<uint4 *>(patch + r * 128 + ((c ^ (r & 7)) << 4)); }
+
+// Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end,
+// uint32_t (&acc)[N], uint8_t *patch) const`: called by the eight epilogue warps, lane by lane with N columns col .. of row
+// row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). All lanes
+// call. Epi::kStream: a tile is one chunk, and its columns come 32 at a time; else all BN / 2 of the warp at once.
 template <int CG, int BN, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s, const Epi epi)
@@ -254,96 +271,143 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             uint32_t it = 0; // slices fetched so far
             bool ok = true;
             // a copy of either CTA of a pair completes at the leader's barrier
+            const uint32_t bytes = CG * (uint32_t)(s.a_rows + s.cols / CG) * (kBK * 2);
             for (int64_t t = first_tile; ok && t < tiles; t += stride) {
                 const Tile tl = tile_of(s, t);
-                const int row = (tl.m * CG + (int)rank) * L::kBM, col = tl.n * BN + (int)rank * L::kBNc;
-                int k = tl.first / s.pairs, q = tl.first - k * s.pairs;
-                for (int i = tl.first; i < tl.last; ++i, ++it) {
-                    const uint32_t st = it % L::kStages, ph = (it / L::kStages) & 1;
-                    if (!bar_wait(smem_u32(&s_empty[st]), ph ^ 1, &s_stop)) {
-                        ok = false;
-                        break;
-                    }
-                    uint32_t full = smem_u32(&s_full[st]);
-                    if (rank == 0) bar_expect(full, CG * L::kStageBytes);
-                    if constexpr (CG == 2) full = map_rank(full, 0);
-                    const uint32_t a = ring + st * L::kStageBytes, b = a + L::kABytes;
-                    const int za = plane_a(s.pairs, q), zb = plane_b(s.pairs, q);
-                    if constexpr (AMN) {
+                const int row = (tl.m * CG + (int)rank) * L::kBM, col = tl.n * s.cols + (int)rank * L::kBNc;
+                for (int c0 = tl.first; ok && c0 < tl.last; c0 += s.chunk) {
+                    const int c1 = min(c0 + s.chunk, tl.last);
+                    for (int q = 0; ok && q < s.pairs; ++q) {
+                        const int za = plane_a(s.pairs, q), zb = plane_b(s.pairs, q);
+                        for (int k = c0; k < c1; ++k, ++it) {
+                            const uint32_t st = it % L::kStages, ph = (it / L::kStages) & 1;
+                            if (!bar_wait(smem_u32(&s_empty[st]), ph ^ 1, &s_stop)) {
+                                ok = false;
+                                break;
+                            }
+                            uint32_t full = smem_u32(&s_full[st]);
+                            if (rank == 0) bar_expect(full, bytes);
+                            if constexpr (CG == 2) full = map_rank(full, 0);
+                            const uint32_t a = ring + st * L::kStageBytes, b = a + L::kABytes;
+                            if constexpr (AMN) {
 #pragma unroll
-                        for (int j = 0; j < L::kBM / 64; ++j) fetch<CG>(a + j * 8192, &map_a, row + j * 64, k * kBK, za, full);
-                    } else {
-                        fetch<CG>(a, &map_a, k * kBK, row, za, full);
-                    }
-                    if constexpr (BMN) {
+                                for (int j = 0; j < L::kBM / 64; ++j) fetch<CG>(a + j * 8192, &map_a, row + j * 64, k * kBK, za, full);
+                            } else {
+                                fetch<CG>(a, &map_a, k * kBK, row, za, full);
+                            }
+                            if constexpr (BMN) {
 #pragma unroll
-                        for (int j = 0; j < L::kBNc / 64; ++j) fetch<CG>(b + j * 8192, &map_b, col + j * 64, k * kBK, zb, full);
-                    } else {
-                        fetch<CG>(b, &map_b, k * kBK, col, zb, full);
-                    }
-                    if (++q == s.pairs) {
-                        q = 0;
-                        ++k;
+                                for (int j = 0; j < L::kBNc / 64; ++j) // (only whole tiles: cols == BN)
+                                    fetch<CG>(b + j * 8192, &map_b, col + j * 64, k * kBK, zb, full);
+                            } else {
+                                fetch<CG>(b, &map_b, k * kBK, col, zb, full);
+                            }
+                        }
                     }
                 }
             }
             if (!ok && rank == 0) // what is in flight still lands in this CTA's shared memory
-                for (uint32_t j = it > (uint32_t)L::kStages ? it - L::kStages : 0; j < it; ++j) {
-                    const uint64_t t0 = now_ns();
-                    while (!bar_try(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1) && now_ns() - t0 < kWaitNs) {}
-                }
+                for (uint32_t j = it > (uint32_t)L::kStages ? it - L::kStages : 0; j < it; ++j)
+                    bar_drain(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1);
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
             const uint32_t type = s.half ? 0u : 1u;
             const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) |
-                                   ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((CG * 128) >> 4) << 24);
-            uint32_t it = 0, n_tile = 0;
+                                   ((uint32_t)(s.cols >> 3) << 17) | ((uint32_t)((CG * 128) >> 4) << 24);
+            uint32_t it = 0, n_chunk = 0;
             bool ok = true;
-            for (int64_t t = first_tile; ok && t < tiles; t += stride, ++n_tile) {
+            for (int64_t t = first_tile; ok && t < tiles; t += stride) {
                 const Tile tl = tile_of(s, t);
-                const uint32_t acc = n_tile & 1, ph = (n_tile >> 1) & 1;
-                if (!bar_wait(smem_u32(&s_free[acc]), ph ^ 1, &s_stop)) break;
-                fence_after();
-                const uint32_t d = tmem + acc * BN;
-                for (int i = tl.first; i < tl.last; ++i, ++it) {
-                    const uint32_t st = it % L::kStages;
-                    if (!bar_wait(smem_u32(&s_full[st]), (it / L::kStages) & 1, &s_stop)) {
-                        ok = false;
-                        break;
-                    }
+                for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
+                    const int slices = (min(c0 + s.chunk, tl.last) - c0) * s.pairs;
+                    const uint32_t acc = n_chunk & 1;
+                    ok = bar_wait(smem_u32(&s_free[acc]), ((n_chunk >> 1) & 1) ^ 1, &s_stop);
+                    if (!ok) break;
                     fence_after();
-                    const uint32_t a = ring + st * L::kStageBytes;
-                    const uint64_t da = operand_desc(a, AMN ? 8192 : 16), db = operand_desc(a + L::kABytes, BMN ? 8192 : 16);
+                    const uint32_t d = tmem + acc * BN;
+                    for (int i = 0; i < slices; ++i, ++it) {
+                        const uint32_t st = it % L::kStages;
+                        ok = bar_wait(smem_u32(&s_full[st]), (it / L::kStages) & 1, &s_stop);
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t a = ring + st * L::kStageBytes;
+                        const uint64_t da = operand_desc(a, AMN ? 8192 : 16), db = operand_desc(a + L::kABytes, BMN ? 8192 : 16);
 #pragma unroll
-                    for (int kk = 0; kk < kBK / 16; ++kk) // 16 summed elements: 32 bytes on (K-major) or two groups of 8 rows
-                        product<CG>(d, da + kk * (AMN ? 128 : 2), db + kk * (BMN ? 128 : 2), idesc, i > tl.first || kk > 0);
-                    commit<CG>(smem_u32(&s_empty[st]));
+                        for (int kk = 0; kk < kBK / 16; ++kk) // 16 summed elements: 32 bytes on (K-major) or two groups of 8 rows
+                            product<CG>(d, da + kk * (AMN ? 128 : 2), db + kk * (BMN ? 128 : 2), idesc, i > 0 || kk > 0);
+                        commit<CG>(smem_u32(&s_empty[st]));
+                    }
+                    if (!ok) break;
+                    commit<CG>(smem_u32(&s_done[acc]));
                 }
-                if (ok) commit<CG>(smem_u32(&s_done[acc]));
             }
             if (s_stop) { // products in flight are waited for before tensor memory is given back
                 commit<CG>(smem_u32(&s_drain));
-                const uint64_t t0 = now_ns();
-                while (!bar_try(smem_u32(&s_drain), 0) && now_ns() - t0 < kWaitNs) {}
+                bar_drain(smem_u32(&s_drain), 0);
             }
         }
     } else {
-        const int w = warp - 2;
-        uint32_t n_tile = 0;
-        for (int64_t t = first_tile; t < tiles; t += stride, ++n_tile) {
+        constexpr int kN = BN / 2; // columns of a warp
+        // the lanes of tensor memory that a warp may read: 32 (its number in the CTA % 4) ..
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * kN);
+        uint8_t *patch = smem_raw + (ring - smem_u32(smem_raw)) + L::kStages * L::kStageBytes + (warp - 2) * kPatchBytes;
+        uint32_t n_chunk = 0;
+        bool ok = true;
+        for (int64_t t = first_tile; ok && t < tiles; t += stride) {
             const Tile tl = tile_of(s, t);
-            const uint32_t acc = n_tile & 1, ph = (n_tile >> 1) & 1;
-            // (one lane's verdict for the warp: the loads from tensor memory are the whole warp's)
-            bool ok = true;
-            if (lane == 0) ok = bar_wait(smem_u32(&s_done[acc]), ph, &s_stop);
-            if (!__shfl_sync(0xffffffffu, (int)ok, 0)) break;
-            fence_after();
-            // (the lanes of tensor memory that a warp may read are 32 (its number in the CTA % 4) ..)
-            epi.template tile<BN>(s, tl, (tl.m * CG + (int)rank) * L::kBM, tl.n * BN, tmem + acc * BN, warp & 3, w >> 2, lane);
-            fence_before();
+            const int row0 = (tl.m * CG + (int)rank) * L::kBM + quarter * 32, col = tl.n * s.cols + half * kN;
+            const int end = min(s.n, (tl.n + 1) * s.cols); // the tile's columns end here
+            if constexpr (Epi::kStream) {
+                const uint32_t a = n_chunk & 1;
+                ok = lane == 0 ? bar_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop) : true;
+                ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+                if (!ok) break;
+                ++n_chunk;
+                fence_after();
+#pragma unroll 1
+                for (int c = 0; c < kN && col + c < end; c += 32) {
+                    uint32_t r[32];
+                    load32(at + a * BN + c, r);
+                    wait_loads();
+                    epi.template finish<32>(s, tl, row0, lane, col + c, end, r, patch);
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[a]), 0) : smem_u32(&s_free[a]));
+            } else {
+            uint32_t acc[kN];
+            for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
+                const uint32_t a = n_chunk & 1;
+                // (one lane's verdict for the warp: the loads from tensor memory are the whole warp's)
+                ok = lane == 0 ? bar_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop) : true;
+                ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+                if (!ok) break;
+                fence_after();
+                if (c0 == tl.first) {
+#pragma unroll
+                    for (int c = 0; c < kN; c += 32)
+                        if (col + c < end) load32(at + a * BN + c, *reinterpret_cast<uint32_t(*)[32]>(&acc[c]));
+                    wait_loads();
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kN; c += 32)
+                        if (col + c < end) {
+                            uint32_t r[32];
+                            load32(at + a * BN + c, r);
+                            wait_loads();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) acc[c + j] = __float_as_uint(__uint_as_float(acc[c + j]) + __uint_as_float(r[j]));
+                        }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[a]), 0) : smem_u32(&s_free[a]));
+            }
+            if (ok) epi.template finish<kN>(s, tl, row0, lane, col, end, acc, patch);
+            }
             __syncwarp();
-            if (lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[acc]), 0) : smem_u32(&s_free[acc]));
         }
     }
     __syncwarp();

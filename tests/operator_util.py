@@ -30,28 +30,35 @@ def softmax_reference(x, w, labels, weights=None, scale=1.0):
     p[torch.arange(n, device=x.device), at] -= 1.0
     p *= g[:, None]
     zero = torch.zeros_like(lse)
-    # a logit: a sum of d products (single precision: 6 d of planes, and 3 x 2^-24 of each product left out)
-    terms = 6 * d + 3 if dt == torch.float32 else d
+    # a logit: a sum of d products. Single precision: of 3 d products of planes; a plane pair is off by 2^-22 (2 STEP) of an
+    # element or 2^-39 of the largest one, either factor, and the product left out is 2^-22 of a term: 8 STEP of it in all
+    single = dt == torch.float32
+    terms = 3 * d + 8 if single else d
     off = (terms * STEP * (X.abs() @ W.abs().T)).amax(1)
+    if single:
+        off = off + 2.0 ** -38 * (X.abs().max() * W.abs().sum(1).max() + W.abs().max() * X.abs().sum(1))
     # lse and loss: the logits' error, exponentials, their sum and the logarithm, the largest logit's rounding when added
     off_lse = torch.where(has, off + (v / 16 + 32) * STEP + 2 * STEP * (lse.abs() + logits.abs().amax(1)), zero)
     off_loss = torch.where(has, 2 * off + (v / 16 + 32) * STEP + 4 * STEP * (loss.abs() + logits.abs().amax(1)), zero)
     # an entry of P: of exp(logit - lse) the two errors and the exponentials' (16 steps); its storage in between (fp16 2^-12,
-    # and of small ones 2^-40 of the largest) and its rounding; fp16: of the lifted value, which may be subnormal
+    # and of small ones 2^-40 of the largest) and its rounding; fp16 and its planes: of the lifted value, which may be subnormal
     gs = g.abs()[:, None]
     rel = (2 * (off + off_lse) + 16 * STEP)[:, None]
-    off_p = soft * gs * rel + p.abs() * (HALF[dt] if dt != torch.float32 else 4 * STEP)
-    if dt != torch.float32:
+    off_p = soft * gs * rel + p.abs() * (4 * STEP if single else HALF[dt])
+    if not single:
         off_p = off_p + soft * gs * 2.0 ** -12 + gs * 2.0 ** -40
-    if dt == torch.float16:
+    if dt != torch.bfloat16:
         off_p = off_p + float(gs.max()) * 2.0 ** -37
     Wa, Xa = W.abs(), X.abs()
     pa = p.abs() + off_p
-    k = 6 if dt == torch.float32 else 1
+    k = 3 if single else 1
     tiny = torch.finfo(dt).smallest_normal * 2 * HALF[dt]
     dx, dw = p @ W, p.T @ X
-    off_dx = off_p @ Wa + k * v * STEP * (pa @ Wa) + HALF[dt] * dx.abs() * (1 + 2 * HALF[dt]) + tiny
-    off_dw = off_p.T @ Xa + k * (n + 64) * STEP * (pa.T @ Xa) + HALF[dt] * dw.abs() * (1 + 2 * HALF[dt]) + tiny
+    off_dx = off_p @ Wa + (k * v + 8) * STEP * (pa @ Wa) + HALF[dt] * dx.abs() * (1 + 2 * HALF[dt]) + tiny
+    off_dw = off_p.T @ Xa + (k * (n + 64) + 8) * STEP * (pa.T @ Xa) + HALF[dt] * dw.abs() * (1 + 2 * HALF[dt]) + tiny
+    if single:
+        off_dx = off_dx + 2.0 ** -38 * Wa.max() * pa.sum(1, keepdim=True)
+        off_dw = off_dw + 2.0 ** -38 * Xa.max() * pa.sum(0)[:, None]
     off_dx = off_dx + HALF[dt] * (off_p @ Wa)  # (the rounding is of the computed value)
     off_dw = off_dw + HALF[dt] * (off_p.T @ Xa)
     off_dx = torch.where(has[:, None], off_dx, torch.zeros_like(off_dx))
