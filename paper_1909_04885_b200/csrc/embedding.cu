@@ -21,7 +21,7 @@ constexpr int kMaxRankN = 4096;   // ids sorted by counting
 constexpr int kTile = 2048;       // entries per CTA of a radix pass
 constexpr int kTileThreads = 512;
 constexpr int kDigits = 1024;
-constexpr int kGroupTiles = 32;   // tiles whose digit counts are added up in advance
+constexpr int kGroupTiles = 16;   // tiles whose digit counts are added up in advance
 constexpr int64_t kTargetThreads = 148 * 1024;
 constexpr int64_t kZeroBytes = 64 * 1024; // of dtable per zeroing CTA
 // What a launch of the sort zeroes beside it: what memory writes in the 8 to 12 us that it takes up to 10^5 entries, and in
@@ -186,12 +186,10 @@ __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__re
 {
     if ((int64_t)blockIdx.x * kTile >= n) return zero_block(zero, (int64_t)blockIdx.x - (n + kTile - 1) / kTile);
     constexpr int kWarps = kTileThreads / 32, kItems = kTile / kTileThreads;
-    extern __shared__ uint32_t smem[];
+    extern __shared__ __align__(16) uint32_t smem[];
     uint32_t(*cnt)[kDigits] = reinterpret_cast<uint32_t(*)[kDigits]>(smem); // [warp][digit]
     __shared__ uint32_t s_scan[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int j = threadIdx.x; j < kWarps * kDigits; j += kTileThreads) smem[j] = 0;
-    __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kTile + (int64_t)warp * (kItems * 32);
     const uint32_t below = (1u << lane) - 1u;
     int32_t key[kItems], dig[kItems];
@@ -202,6 +200,27 @@ __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__re
         key[it] = i < n ? (raw ? key_of(in[i], rows, nullptr) : in[i]) : 0;
         dig[it] = i < n ? (key[it] >> shift) & (digits - 1) : -1;
     }
+    // where a digit's entries of this tile begin: digits in front (scan of the totals), groups and tiles in front. Two digits
+    // per thread, fetched before the ranking so that its loads are on their way meanwhile.
+    static_assert(kDigits <= 2 * kTileThreads, "two digits per thread");
+    const int g = blockIdx.x / kGroupTiles, d0 = threadIdx.x * 2;
+    uint32_t tot[2] = {0, 0}, own[2] = {0, 0};
+    if (d0 < digits) { // (digits: an even number)
+        const uint2 t2 = *reinterpret_cast<const uint2 *>(total + d0);
+        tot[0] = t2.x, tot[1] = t2.y;
+#pragma unroll 8
+        for (int j = 0; j < g; ++j) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(group + (int64_t)j * digits + d0);
+            own[0] += x.x, own[1] += x.y;
+        }
+#pragma unroll 8
+        for (int j = g * kGroupTiles; j < (int)blockIdx.x; ++j) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(hist + (int64_t)j * digits + d0);
+            own[0] += x.x, own[1] += x.y;
+        }
+    }
+    for (int j = threadIdx.x; j < kWarps * kDigits / 4; j += kTileThreads) reinterpret_cast<uint4 *>(smem)[j] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
 #pragma unroll
     for (int it = 0; it < kItems; ++it) {
         const int d = dig[it];
@@ -211,21 +230,6 @@ __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__re
         if (d >= 0 && (peers & below) == 0u) cnt[warp][d] = before + __popc(peers);
         __syncwarp();
         rank[it] = before + __popc(peers & below);
-    }
-    // where a digit's entries of this tile begin: digits in front (scan of the totals), groups and tiles in front
-    const int g = blockIdx.x / kGroupTiles;
-    uint32_t tot[2], own[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int d = threadIdx.x * 2 + k;
-        tot[k] = own[k] = 0;
-        if (d < digits) {
-            tot[k] = total[d];
-#pragma unroll 8
-            for (int j = 0; j < g; ++j) own[k] += group[(int64_t)j * digits + d];
-#pragma unroll 8
-            for (int j = g * kGroupTiles; j < (int)blockIdx.x; ++j) own[k] += hist[(int64_t)j * digits + d];
-        }
     }
     uint32_t inc = tot[0] + tot[1];
 #pragma unroll
@@ -239,7 +243,7 @@ __global__ void __launch_bounds__(kTileThreads) k_id_scatter(const int32_t *__re
     for (int w = 0; w < warp; ++w) start += s_scan[w];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int d = threadIdx.x * 2 + k;
+        const int d = d0 + k;
         if (d < digits) {
             uint32_t run = start + own[k];
 #pragma unroll
@@ -377,7 +381,7 @@ __global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__rest
 // Adds the partial sums of the runs that cross windows, in order. A warp looks at the window where a run may begin; it adds
 // a few partial sums itself, many are left to the CTA: its groups of threads take consecutive windows each, and their
 // sums are added in order.
-constexpr int kWarpJoin = 32; // partial sums that a warp takes
+constexpr int kWarpJoin = 32; // vectors per lane that a warp takes (16384 entries of 4096 bf16: 44 us with 32 partial sums of any length)
 
 template <typename T, int E>
 __global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restrict__ table, int64_t ld_t)
@@ -399,7 +403,7 @@ __global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restric
                 // windows w + 1 .. the one with the run's last entry hold the rest
                 const int64_t end = first_not_below(s.keys + e1, (int32_t)(s.n - e1), k + 1) + e1;
                 count = (end - 1) / s.window - w + 1;
-                if (count <= kWarpJoin) {
+                if (count * ((c_end - c_begin + 31) / 32) <= kWarpJoin) {
                     for (int c = c_begin + lane; c < c_end; c += 32) {
                         float acc[E];
 #pragma unroll
@@ -489,7 +493,7 @@ IdPlan make_plan(int64_t n, int64_t rows, int64_t cols)
     if (n > kMaxRankN) {
         const int bits = log2_up(rows + 1);
         p.passes = (int)std::max<int64_t>(1, ceil_div(bits, 10));
-        p.digit_bits = (int)ceil_div(bits, p.passes);
+        p.digit_bits = (int)std::max<int64_t>(1, ceil_div(bits, p.passes)); // (rows + 1 keys: two at least)
         p.tiles = ceil_div(n, kTile);
         p.groups = ceil_div(p.tiles, kGroupTiles);
         const size_t digits = (size_t)1 << p.digit_bits;
@@ -572,11 +576,9 @@ cudaError_t lookup(const chicle_dense_t &t, const int32_t *ids, float scale, con
     const int64_t per = 256 >> tpr_log;
     // four rows per thread where that leaves every SM its CTAs
     if (ceil_div(o.rows, per * 4) * slabs >= kSms * 8)
-        k_lookup<T, E, 4><<<dim3((unsigned)ceil_div(o.rows, per * 4), slabs), 256, 0, s>>>(
-            (const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
+        k_lookup<T, E, 4><<<dim3((unsigned)ceil_div(o.rows, per * 4), slabs), 256, 0, s>>>((const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
     else
-        k_lookup<T, E, 1><<<dim3((unsigned)ceil_div(o.rows, per), slabs), 256, 0, s>>>(
-            (const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
+        k_lookup<T, E, 1><<<dim3((unsigned)ceil_div(o.rows, per), slabs), 256, 0, s>>>((const T *)t.data, t.ld, (int32_t)t.rows, ids, o.rows, vecs, tpr_log, scale, (T *)o.data, o.ld, status);
     return cudaGetLastError();
 }
 

@@ -4,10 +4,10 @@
 //   l_iv = x_i . w_v        lse_i = log sum_v exp(l_iv)        loss_i = lse_i - l_{i, y_i}
 //   p_iv = g_i (exp(l_iv - lse_i) - [v = y_i])                 dX = P W,  dW = P^T X
 //
-// The logits are never held as a whole. The loss alone keeps, per row and 128 (or 64) classes, the largest logit and the sum
+// The logits are never held as a whole. The loss alone keeps, per row and block of classes (a warp's columns of a tile), the largest logit and the sum
 // of exponentials relative to it; a second kernel joins them. For the gradients the rows are taken in pieces of about two
-// gigabytes of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the largest of the row in its 128
-// classes) as fp16, scaled by 2^15 so that what is 2^-29 of the tile's largest still has all its bits; an elementwise
+// gigabytes of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the largest of the row in the
+// block) as fp16, scaled by 2^15 so that what is 2^-29 of the tile's largest still has all its bits; an elementwise
 // pass turns the piece into P in place, and two products take dX and the piece's share of dW from it. So the
 // logits are computed once: 6 n V d operations, against 8 where they are computed again for the gradient, for 6 bytes of traffic
 // per logit (at d = 4096 a third of the products' time against a twentieth).
@@ -59,7 +59,7 @@ enum { kLift, kInvLift, kLiftX, kInvX, kLiftW, kInvW, kScales };
 // Reduces a tile of logits to (largest, sum of exponentials) per row and N classes, keeps the label's logit, and
 // writes the exponentials for the gradients: StoreT void (loss alone), half, or float (single precision).
 template <typename StoreT> struct LogitsEpilogue {
-    static constexpr bool kStream = false;
+    static constexpr int kStep = 0;
     const int32_t *labels; // rows of this piece
     float2 *stats;         // [block of N classes][rows]
     float *label_logit;    // [rows]
@@ -100,7 +100,7 @@ template <typename StoreT> struct LogitsEpilogue {
         const float ref = top == -INFINITY ? 0.f : top;
         uint64_t sum[2] = {0, 0}; // pairs of floats
         const uint64_t back = pair_of(-ref, -ref), to_log2 = pair_of(kLog2e * factor, kLog2e * factor);
-        constexpr int kWidth = sizeof(StoreT) >= 2 ? 128 / (int)sizeof(StoreT) : N; // columns of a patch
+        constexpr int kWidth = sizeof(StoreT) >= 2 ? 64 / (int)sizeof(StoreT) : N; // columns of a patch
         constexpr int kPer = sizeof(StoreT) >= 2 ? 16 / (int)sizeof(StoreT) : 8;    // and of a piece
 #pragma unroll
         for (int g = 0; g < N; g += kWidth) {
@@ -128,18 +128,17 @@ template <typename StoreT> struct LogitsEpilogue {
             }
             if constexpr (sizeof(StoreT) >= 2) {
                 __syncwarp();
-                const int piece = lane & 7, col = c0 + g + piece * kPer;
-                StoreT *dst = store + (int64_t)(row0 + (lane >> 3)) * ld + col;
-#pragma unroll 2
-                for (int i = 0; i < 8; ++i) { // (ld: a multiple of 8, what lies behind the last class is not read)
-                    const int rr = 4 * i + (lane >> 3);
-                    if (row0 + rr < s.m && col < end) *reinterpret_cast<uint4 *>(dst + (int64_t)(4 * i) * ld) = *tc::patch_at(patch, rr, piece);
+                const int piece = lane & 3, col = c0 + g + piece * kPer;
+                StoreT *dst = store + (int64_t)(row0 + (lane >> 2)) * ld + col;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { // (ld: a multiple of 64, what lies behind the last class is not read)
+                    const int rr = 8 * i + (lane >> 2);
+                    if (row0 + rr < s.m && col < end) *reinterpret_cast<uint4 *>(dst + (int64_t)(8 * i) * ld) = *tc::patch_at(patch, rr, piece);
                 }
             }
         }
         // NaN: fmaxf passes over it, the sum does not
-        // (blocks: two per tile, whether the second has columns or not)
-        if (live && c0 < end) stats[(int64_t)(tl.n * 2 + (c0 - tl.n * s.cols >= N)) * s.m + row] = make_float2(top * factor, (low_of(sum[0]) + low_of(sum[1])) + (high_of(sum[0]) + high_of(sum[1])));
+        if (live && c0 < end) stats[(int64_t)(tl.n * s.parts + (c0 - tl.n * s.cols) / N) * s.m + row] = make_float2(top * factor, (low_of(sum[0]) + low_of(sum[1])) + (high_of(sum[0]) + high_of(sum[1])));
     }
 };
 
@@ -157,7 +156,7 @@ template <> __device__ __forceinline__ __half from_float<__half>(float v) { retu
 // Where a tile of a gradient goes. With splits: to `partial`, one plane per split. Else sum = (add ? *add : 0) + tile; to
 // `keep` (fp32, for the pieces that follow) or to `out`.
 template <typename OutT> struct GradEpilogue {
-    static constexpr bool kStream = sizeof(OutT) == 2; // single precision: sums in chunks
+    static constexpr int kStep = 32;
     OutT *out;
     int64_t ld;
     float *partial;          // [split][m][n]
@@ -179,18 +178,18 @@ template <typename OutT> struct GradEpilogue {
         const bool quads = (s.n & 3) == 0; // fp32 rows of n: 16-byte pieces
         const bool quads_out = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * sizeof(OutT))) & (4 * sizeof(OutT) - 1)) == 0;
 #pragma unroll
-        for (int g = 0; g < N; g += 32) {
+        for (int g = 0; g < N; g += 16) {
             if (c0 + g >= end) break;
             __syncwarp();
 #pragma unroll
-            for (int c = 0; c < 8; ++c) *tc::patch_at(patch, lane, c) = make_uint4(r[g + 4 * c], r[g + 4 * c + 1], r[g + 4 * c + 2], r[g + 4 * c + 3]);
+            for (int c = 0; c < 4; ++c) *tc::patch_at(patch, lane, c) = make_uint4(r[g + 4 * c], r[g + 4 * c + 1], r[g + 4 * c + 2], r[g + 4 * c + 3]);
             __syncwarp();
-            const int col = c0 + g + 4 * (lane & 7);
+            const int col = c0 + g + 4 * (lane & 3);
 #pragma unroll 2
-            for (int i = 0; i < 8; ++i) {
-                const int rr = 4 * i + (lane >> 3), row = row0 + rr;
+            for (int i = 0; i < 4; ++i) {
+                const int rr = 8 * i + (lane >> 2), row = row0 + rr;
                 if (row >= s.m || col >= end) continue;
-                float4 v = *reinterpret_cast<const float4 *>(tc::patch_at(patch, rr, lane & 7));
+                float4 v = *reinterpret_cast<const float4 *>(tc::patch_at(patch, rr, lane & 3));
                 if ((zeros >> rr) & 1u) v = make_float4(0.f, 0.f, 0.f, 0.f);
                 const int64_t at = (int64_t)row * s.n + col;
                 if (col + 4 <= s.n && (whole ? quads : quads_out) && (!src || quads)) {
@@ -306,65 +305,78 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
     }
 }
 
-// Exponentials to P, 8 classes per thread: in place for 16-bit operands, from fp32 to two fp16 planes for single precision.
-template <typename PT, bool kWide>
+// Exponentials to P, kSteps times 8 classes of a row per thread: in place for 16-bit operands, from fp32 to two fp16 planes for
+// single precision. Bound by memory: 8192 x 131072 in 640 us, 6.7 TB/s (with one step 850; 10000 x 1000: one step 13 us, four
+// 26, most of whose threads have nothing to do).
+template <typename PT, bool kWide, int kSteps>
 __global__ void __launch_bounds__(256)
 k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, int32_t classes, const float2 *__restrict__ stats,
                 const float2 *__restrict__ norm, const float *__restrict__ loss, const int32_t *__restrict__ labels,
                 const float *__restrict__ weights, float scale, const float *__restrict__ lift, int block_log)
 {
     const int row = blockIdx.y;
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c >= classes) return;
+    const int c0 = (blockIdx.x * kSteps * 256 + threadIdx.x) * 8;
     const int32_t y = labels[row];
     const bool has = (uint32_t)y < (uint32_t)classes;
-    float v[8];
+    uint4 in[kSteps][kWide ? 2 : 1];
+    float ref[kSteps];
     if (has) {
-        float g = weights ? weights[row] * scale : scale;
-        if (lift) g *= *lift;
-        // relative to the largest logit: lse has lost the bits that the two share
-        const float2 of = norm[row];
-        const float f = exp2f((stats[(int64_t)(c >> block_log) * n + row].x - of.x) * kLog2e) * of.y * (kWide ? 1.f : 1.f / kStoreScale) * g;
-        if constexpr (kWide) {
-            const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(store) + (int64_t)row * ld + c);
-            const float4 a = src[0], b = src[1];
-            v[0] = a.x * f, v[1] = a.y * f, v[2] = a.z * f, v[3] = a.w * f;
-            v[4] = b.x * f, v[5] = b.y * f, v[6] = b.z * f, v[7] = b.w * f;
-        } else {
-            const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const __half *>(store) + (int64_t)row * ld + c);
-            const __half2 *h = reinterpret_cast<const __half2 *>(&q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 t = __half22float2(h[j]);
-                v[2 * j] = t.x * f;
-                v[2 * j + 1] = t.y * f;
+        for (int k = 0; k < kSteps; ++k) {
+            const int c = c0 + k * 2048;
+            if (c >= classes) break;
+            if constexpr (kWide) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const float *>(store) + (int64_t)row * ld + c);
+                in[k][0] = src[0], in[k][1] = src[1];
+            } else {
+                in[k][0] = *reinterpret_cast<const uint4 *>(static_cast<const __half *>(store) + (int64_t)row * ld + c);
             }
+            ref[k] = stats[(int64_t)(c >> block_log) * n + row].x;
         }
-        if (y >= c && y < c + 8) {
-            const float at = g * expm1f(-loss[row]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (y - c == j) v[j] = at;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
     }
-    alignas(16) PT q[8];
-    if constexpr (kWide) {
+    float g = weights ? weights[row] * scale : scale;
+    if (lift) g *= *lift;
+    const float2 of = norm[row]; // relative to the largest logit: lse has lost the bits that the two share
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kSteps; ++k) {
+        const int c = c0 + k * 2048;
+        if (c >= classes) break;
+        float v[8];
+        if (has) {
+            const float f = exp2f((ref[k] - of.x) * kLog2e) * of.y * (kWide ? 1.f : 1.f / kStoreScale) * g;
+            if constexpr (kWide) {
+                const float *e = reinterpret_cast<const float *>(in[k]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = e[j] * f;
+            } else {
+                const __half2 *h = reinterpret_cast<const __half2 *>(in[k]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 t = __half22float2(h[j]);
+                    v[2 * j] = t.x * f;
+                    v[2 * j + 1] = t.y * f;
+                }
+            }
+            if (y >= c && y < c + 8) {
+                const float at = g * expm1f(-loss[row]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (y - c == j) v[j] = at;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        }
+        alignas(16) PT q[8];
+#pragma unroll
+        for (int w = 0; w < (kWide ? 2 : 1); ++w) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 q[j] = from_float<PT>(v[j]);
                 v[j] -= (float)q[j];
             }
-            *reinterpret_cast<uint4 *>(p + k * plane + (int64_t)row * ld + c) = *reinterpret_cast<const uint4 *>(q);
+            *reinterpret_cast<uint4 *>(p + w * plane + (int64_t)row * ld + c) = *reinterpret_cast<const uint4 *>(q);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = from_float<PT>(v[j]);
-        *reinterpret_cast<uint4 *>(p + (int64_t)row * ld + c) = *reinterpret_cast<const uint4 *>(q);
     }
 }
 
@@ -420,23 +432,34 @@ __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, in
     const float *src = of_x ? x : w;
     const int64_t ld = of_x ? ld_x : ld_w, rows = of_x ? n : classes;
     const bool quads = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && (ld & 3) == 0 && (d & 3) == 0;
-    const int per = quads ? d / 4 : d;
-    const int64_t all = rows * per;
     float top = 0.f;
     auto take = [&](float v) {
         v = fabsf(v);
         if (v < INFINITY) top = fmaxf(top, v);
     };
-#pragma unroll 4
-    for (int64_t i = (int64_t)(blockIdx.x % kMaxBlocks) * 256 + threadIdx.x; i < all; i += (int64_t)kMaxBlocks * 256) {
-        const int64_t row = i / per;
-        const int c = (int)(i - row * per);
-        if (of_x && (uint32_t)labels[row] >= (uint32_t)classes) continue;
-        if (quads) {
-            const float4 v = *reinterpret_cast<const float4 *>(src + row * ld + 4 * c);
+    const int64_t first = (int64_t)(blockIdx.x % kMaxBlocks) * 256 + threadIdx.x, step = (int64_t)kMaxBlocks * 256;
+    if (!of_x && quads && ld == d) { // no rows to be told apart: 134 MB in 24 us instead of 47
+        const float4 *flat = reinterpret_cast<const float4 *>(src);
+        const int64_t all = rows * (d / 4);
+#pragma unroll 8
+        for (int64_t i = first; i < all; i += step) {
+            const float4 v = flat[i];
             take(v.x), take(v.y), take(v.z), take(v.w);
-        } else {
-            take(src[row * ld + c]);
+        }
+    } else {
+        const int per = quads ? d / 4 : d;
+        const int64_t all = rows * per;
+#pragma unroll 4
+        for (int64_t i = first; i < all; i += step) {
+            const int64_t row = i / per;
+            const int c = (int)(i - row * per);
+            if (of_x && (uint32_t)labels[row] >= (uint32_t)classes) continue;
+            if (quads) {
+                const float4 v = *reinterpret_cast<const float4 *>(src + row * ld + 4 * c);
+                take(v.x), take(v.y), take(v.z), take(v.w);
+            } else {
+                take(src[row * ld + c]);
+            }
         }
     }
 #pragma unroll
@@ -521,7 +544,7 @@ bool make_map(CUtensorMap *map, const Operand &o, bool half, int box_cols, int b
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, int BN, bool AMN, bool BMN, class Epi>
+template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
 cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int cols, const Epi &epi, cudaStream_t stream)
 {
     using L = tc::Layout<CG, BN>;
@@ -531,7 +554,8 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int 
     s.m_tiles = (int32_t)ceil_div(s.m, CG * L::kBM);
     s.n_tiles = (int32_t)ceil_div(s.n, cols);
     s.cols = cols;
-    auto *kernel = tc::k_product<CG, BN, AMN, BMN, Epi>;
+    auto *kernel = tc::k_product<CG, BN, AMN, BMN, kChunked, Epi>;
+    s.parts = tc::kEpiWarps / 4;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)s.m_tiles * s.n_tiles * s.splits;
@@ -541,12 +565,10 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int 
     cfg.dynamicSmemBytes = L::kSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
-    if (CG == 2) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim = {2, 1, 1};
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-    }
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {CG, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, ma, mb, s, epi);
 }
 
@@ -559,29 +581,37 @@ int tile_rows(int64_t m) { return pairs_of_ctas(m) ? 256 : 128; }
 
 // The loss of few rows is bound by the stream of W: there the tile has as many columns as share the classes out most evenly
 // (131072 classes on 148 SMs: four turns of 224 instead of 256, and nothing left to do in the fifth).
-int logit_columns(int64_t rows, int64_t classes, bool grad)
+int logit_columns(int64_t rows, int64_t classes, int parts, bool grad)
 {
     const int most = tile_columns(classes);
     if (grad || most == 128 || pairs_of_ctas(rows)) return most;
     int best = most;
-    for (int c = most - 32; c > most / 2; c -= 32)
+    for (int c = most - 16; c > most / parts * (parts - 1); c -= 16)
         if (ceil_div(ceil_div(classes, c), kSms) * (c + 8) < ceil_div(ceil_div(classes, best), kSms) * (best + 8)) best = c;
     return best;
 }
 
-// Pairs of (largest, sum) per row: one for each half of a tile that has columns.
-int64_t blocks_of(int64_t classes, int cols)
+// Pairs of (largest, sum) per row: one for each part of a tile that has columns.
+int64_t blocks_of(int64_t classes, int cols, int parts)
 {
     const int64_t tiles = ceil_div(classes, cols), last = classes - (tiles - 1) * cols;
-    return 2 * (tiles - 1) + (last > tile_columns(classes) / 2 ? 2 : 1);
+    return parts * (tiles - 1) + ceil_div(last, tile_columns(classes) / parts);
 }
 
-template <bool AMN, bool BMN, class Epi>
+template <bool AMN, bool BMN, bool kChunked, class Epi>
 cudaError_t run_product(const Operand &a, const Operand &b, const tc::Shape &s, int cols, const Epi &epi, cudaStream_t stream)
 {
     if (tile_columns(s.n) == 128)
-        return pairs_of_ctas(s.m) ? launch_product<2, 128, AMN, BMN>(a, b, s, cols, epi, stream) : launch_product<1, 128, AMN, BMN>(a, b, s, cols, epi, stream);
-    return pairs_of_ctas(s.m) ? launch_product<2, 256, AMN, BMN>(a, b, s, cols, epi, stream) : launch_product<1, 256, AMN, BMN>(a, b, s, cols, epi, stream);
+        return pairs_of_ctas(s.m) ? launch_product<2, 128, AMN, BMN, kChunked>(a, b, s, cols, epi, stream)
+                                  : launch_product<1, 128, AMN, BMN, kChunked>(a, b, s, cols, epi, stream);
+    return pairs_of_ctas(s.m) ? launch_product<2, 256, AMN, BMN, kChunked>(a, b, s, cols, epi, stream)
+                              : launch_product<1, 256, AMN, BMN, kChunked>(a, b, s, cols, epi, stream);
+}
+
+template <class Epi>
+cudaError_t run_logits(const Operand &a, const Operand &b, const tc::Shape &s, int cols, const Epi &epi, cudaStream_t stream)
+{
+    return s.k_steps > s.chunk ? run_product<false, false, true>(a, b, s, cols, epi, stream) : run_product<false, false, false>(a, b, s, cols, epi, stream);
 }
 
 int element_size(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
@@ -623,6 +653,8 @@ struct Plan {
     bool pack_x, pack_w;
     int64_t pitch_d, ld_v;
     int64_t piece;     // rows per piece
+    int logit_chunk, grad_chunk; // slices per accumulator
+    int cols, parts;   // of the logits' tiles
     int splits_x, splits_w;
     // offsets into the workspace
     size_t x, w, stats, label_logit, norm, store, p, acc, partial, scales, largest, total;
@@ -641,6 +673,13 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     // rows of whole 128-byte lines: a row of a bulk copy that straddles two takes two requests
     p.pitch_d = (p.d + 63) / 64 * 64;
     p.ld_v = (p.v + 63) / 64 * 64;
+    // Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential
+    // takes on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 512:
+    // 7e-7, 256: 4e-7); all of them where a gradient is rounded to 16 bits in the end.
+    p.logit_chunk = (p.wide ? 512 : 1024) / tc::kBK;
+    p.grad_chunk = p.wide ? 512 / tc::kBK : INT32_MAX / 2;
+    p.parts = tc::kEpiWarps / 4;
+    p.cols = logit_columns(p.n, p.v, p.parts, grad);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -657,7 +696,7 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     }
     if (p.pack_x) p.x = take((size_t)p.planes * p.n * p.pitch_d * 2);
     if (p.pack_w) p.w = take((size_t)p.planes * p.v * p.pitch_d * 2);
-    p.stats = take((size_t)(blocks_of(p.v, logit_columns(p.piece, p.v, grad)) * p.piece) * sizeof(float2));
+    p.stats = take((size_t)(blocks_of(p.v, p.cols, p.parts) * p.piece) * sizeof(float2));
     p.label_logit = take((size_t)p.piece * 4);
     if (grad) p.norm = take((size_t)p.piece * sizeof(float2));
     if (grad) {
@@ -723,12 +762,6 @@ Operand operand_of(const chicle_dense_t &src, const void *packed, bool is_packed
     return o;
 }
 
-// Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential takes
-// on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 256: 4e-7); all
-// of them where a gradient is rounded to 16 bits in the end.
-int logit_chunk(const Plan &p) { return (p.wide ? 512 : 1024) / tc::kBK; }
-int grad_chunk(const Plan &p) { return p.wide ? 512 / tc::kBK : INT32_MAX / 2; }
-
 tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int chunk, int splits, int group, uint32_t *status)
 {
     tc::Shape s{};
@@ -743,10 +776,10 @@ tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int chunk, in
     return s;
 }
 
-cudaError_t join_blocks(const Plan &p, const float2 *stats, int cols, int64_t rows, const int32_t *labels, const float *label_logit, float *loss,
+cudaError_t join_blocks(const Plan &p, const float2 *stats, int64_t rows, const int32_t *labels, const float *label_logit, float *loss,
                         float *lse, float2 *norm, uint32_t *status, cudaStream_t s)
 {
-    const int blocks = (int)blocks_of(p.v, cols);
+    const int blocks = (int)blocks_of(p.v, p.cols, p.parts);
     if (rows >= 32 * 64)
         k_join_blocks<32><<<(unsigned)ceil_div(rows, 32), 512, 0, s>>>(stats, blocks, (int32_t)rows, labels, (int32_t)p.v, label_logit, loss, lse, norm, status);
     else if (rows >= 8)
@@ -766,12 +799,11 @@ int group_of(int64_t k, int planes, int rows_per_tile)
 template <typename OutT>
 cudaError_t gradient(const Plan &p, const Operand &a, const Operand &b, bool of_x, tc::Shape s, GradEpilogue<OutT> epi, cudaStream_t stream)
 {
-    cudaError_t e = of_x ? run_product<false, true>(a, b, s, tile_columns(s.n), epi, stream) : run_product<true, true>(a, b, s, tile_columns(s.n), epi, stream);
+    cudaError_t e = of_x ? run_product<false, true, sizeof(OutT) == 4>(a, b, s, tile_columns(s.n), epi, stream) : run_product<true, true, sizeof(OutT) == 4>(a, b, s, tile_columns(s.n), epi, stream);
     if (e == cudaSuccess && s.splits > 1) {
         const int64_t all = (int64_t)s.m * s.n;
         auto *join = (s.n & 3) == 0 ? k_join_splits<OutT, 4> : k_join_splits<OutT, 1>;
-        join<<<(unsigned)std::min<int64_t>(ceil_div(all, 1024), kSms * 8), 256, 0, stream>>>(
-            epi.partial, s.splits, s.m, s.n, epi.add, epi.keep, epi.out, epi.ld, epi.scale, epi.scale_b, epi.labels, epi.classes);
+        join<<<(unsigned)std::min<int64_t>(ceil_div(all, 1024), kSms * 8), 256, 0, stream>>>(epi.partial, s.splits, s.m, s.n, epi.add, epi.keep, epi.out, epi.ld, epi.scale, epi.scale_b, epi.labels, epi.classes);
         e = cudaGetLastError();
     }
     return e;
@@ -788,7 +820,6 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
     if (e == cudaSuccess) e = pack(X, ws + p.x, p, labels, scales + kLiftX, stream);
     if (e == cudaSuccess && p.pack_w) e = pack(W, ws + p.w, p, nullptr, scales + kLiftW, stream);
     const Operand w = operand_of(W, ws + p.w, p.pack_w, p);
-    const int cols = logit_columns(p.n, p.v, true);
     for (int64_t r0 = 0; e == cudaSuccess && r0 < p.n; r0 += p.piece) {
         const int64_t rows = std::min(p.piece, p.n - r0);
         Operand x = operand_of(X, ws + p.x, true, p);
@@ -800,22 +831,24 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         StoreT *store = reinterpret_cast<StoreT *>(ws + p.store);
         PT *prob = reinterpret_cast<PT *>(ws + p.p);
         const LogitsEpilogue<StoreT> le{labels + r0, stats, label_logit, store, p.ld_v, kWide ? scales : nullptr};
-        e = run_product<false, false>(x, w, shape_of(p, rows, p.v, p.d, logit_chunk(p), 1, group_of(p.d, p.planes, tile_rows(p.n)), status), cols, le, stream);
-        if (e == cudaSuccess) e = join_blocks(p, stats, cols, rows, labels + r0, label_logit, loss + r0, lse + r0, norm, status, stream);
+        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), status), p.cols, le, stream);
+        if (e == cudaSuccess) e = join_blocks(p, stats, rows, labels + r0, label_logit, loss + r0, lse + r0, norm, status, stream);
         if (e != cudaSuccess) break;
         Operand q;
         q.data = prob;
         q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.planes;
+        const int steps = p.v >= 8192 ? 4 : 1;
+        auto *probabilities = steps == 4 ? k_probabilities<PT, kWide, 4> : k_probabilities<PT, kWide, 1>;
         for (int64_t y = 0; y < rows; y += 65535)
-            k_probabilities<PT, kWide><<<dim3((unsigned)ceil_div(p.v, 2048), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(
-                store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
-                labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr, cols == 128 ? 6 : 7);
+            probabilities<<<dim3((unsigned)ceil_div(p.v, 2048 * steps), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
+                labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr,
+                __builtin_ctz(tile_columns(p.v) / p.parts));
         if ((e = cudaGetLastError()) != cudaSuccess) break;
         const float *back = scales ? scales + kInvLift : nullptr;
         float *partial = reinterpret_cast<float *>(ws + p.partial);
         GradEpilogue<T> ex{static_cast<T *>(dX.data) + r0 * dX.ld, dX.ld, p.splits_x > 1 ? partial : nullptr, nullptr, nullptr, back,
                            kWide ? scales + kInvW : nullptr, labels + r0, (int32_t)p.v};
-        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, grad_chunk(p), p.splits_x, 8, status), ex, stream);
+        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, p.grad_chunk, p.splits_x, 8, status), ex, stream);
         if (e != cudaSuccess) break;
         // dW over the pieces: the sums stay in fp32 until the last
         const bool first = r0 == 0, last = r0 + rows >= p.n;
@@ -825,7 +858,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         if (!last) ew.keep = acc;
         const int splits = (int)std::min<int64_t>(p.splits_w, ceil_div(rows, tc::kBK));
         if (splits > 1) ew.partial = partial;
-        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, grad_chunk(p), splits, 8, status), ew, stream);
+        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, p.grad_chunk, splits, 8, status), ew, stream);
     }
     return e;
 }
@@ -906,12 +939,11 @@ extern "C" chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, co
     if (e == cudaSuccess && p.pack_w) e = pack(*W, ws + p.w, p, nullptr, scales + kLiftW, s);
     float2 *stats = reinterpret_cast<float2 *>(ws + p.stats);
     float *label_logit = reinterpret_cast<float *>(ws + p.label_logit);
-    const int cols = logit_columns(p.n, p.v, false);
     const LogitsEpilogue<NoStore> le{dev_labels, stats, label_logit, nullptr, 0, scales};
     if (e == cudaSuccess)
-        e = run_product<false, false>(operand_of(*X, ws + p.x, p.pack_x, p), operand_of(*W, ws + p.w, p.pack_w, p),
-                                                 shape_of(p, p.n, p.v, p.d, logit_chunk(p), 1, group_of(p.d, p.planes, tile_rows(p.n)), dev_status), cols, le, s);
-    if (e == cudaSuccess) e = join_blocks(p, stats, cols, p.n, dev_labels, label_logit, dev_loss, dev_lse, nullptr, dev_status, s);
+        e = run_logits(operand_of(*X, ws + p.x, p.pack_x, p), operand_of(*W, ws + p.w, p.pack_w, p),
+                                                 shape_of(p, p.n, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), dev_status), p.cols, le, s);
+    if (e == cudaSuccess) e = join_blocks(p, stats, p.n, dev_labels, label_logit, dev_loss, dev_lse, nullptr, dev_status, s);
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
 }
 

@@ -3,7 +3,7 @@
 //
 // One CTA (CG = 1: tiles of 128 x BN) or a pair of CTAs on two SMs (CG = 2: tiles of 256 x BN, each CTA holds half of
 // either operand) walks tiles in a fixed order. Warp 0 fetches 64-wide slices of both operands with tiled bulk copies
-// into a ring of stages, one thread of warp 1 issues the products (the pair's leader for both CTAs), eight warps read
+// into a ring of stages, one thread of warp 1 issues the products (the pair's leader for both CTAs), the other warps read
 // the accumulators back and finish the tile while the next tile's products run into the other half of tensor memory.
 //
 // Either operand may have the summed index contiguous ("K-major", rows of 64 elements) or the other one
@@ -29,15 +29,15 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "chicle_internal.cuh"
+#include "operators.cuh"
 
 namespace chicle {
 namespace tc {
 
 constexpr int kBK = 64;              // summed elements per stage: 128 bytes, one swizzle span
-constexpr int kThreads = 320;        // copy warp, product warp, 8 epilogue warps
-constexpr int kEpiWarps = 8;
-constexpr uint32_t kPatchBytes = 4096; // shared memory of an epilogue warp: 32 rows of 128 bytes
+constexpr int kEpiWarps = 8;                 // (sixteen with half the columns each: products of 4096 terms 6 % slower, of 64 the same)
+constexpr int kThreads = 64 + 32 * kEpiWarps; // and a copy warp, a product warp
+constexpr uint32_t kPatchBytes = 2048;  // shared memory of an epilogue warp: 32 rows of 64 bytes
 constexpr long long kWaitClocks = 6000000000ll; // some seconds
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -77,6 +77,16 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
             return false;
         }
     }
+}
+// The epilogue's warps wait for an accumulator: one of their threads looks, the others sleep at a barrier (threads that all
+// look take power and issue slots from the products: dX of 2048 rows, 32768 classes and 4096 columns took 410 us, 396 so). All of
+// them get the same answer.
+__device__ __forceinline__ bool epilogue_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped, volatile uint32_t *answer, bool looks)
+{
+    if (looks) *answer = bar_wait(bar, parity, stopped);
+    __syncwarp();
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+    return *answer != 0;
 }
 // For what is in flight when a CTA stops.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
@@ -161,9 +171,10 @@ struct Shape {
     int32_t m, n;           // rows and columns of C
     int32_t m_tiles, n_tiles;
     int32_t a_rows;         // rows of A that a copy brings: 128, or fewer where C has no more (K-major A, CG = 1 only)
-    int32_t cols;           // columns per tile: BN, or fewer (a multiple of 32, CG = 1 only)
+    int32_t cols;           // columns per tile: BN, or fewer (a multiple of 16, CG = 1 only; every epilogue warp keeps some)
     int32_t k_steps;        // slices of kBK of the summed index (per pair of planes)
     int32_t pairs;          // 1, or 3 for single precision
+    int32_t parts;          // epilogue warps that share a tile's columns
     int32_t chunk;          // slices summed in one accumulator
     int32_t splits;         // the summed index is cut into so many pieces, each a tile of its own
     int32_t group;          // m tiles walked together before the next column of tiles
@@ -209,16 +220,16 @@ template <int CG, int BN> struct Layout {
     static_assert(kSmem <= 227u * 1024u - 512u, "shared memory of an SM");
 };
 
-// 16-byte piece `c` of row `r` of a warp's patch: rows of 128 bytes whose pieces are exchanged so that both a piece of all rows and
-// whole rows are free of bank conflicts. Results go through it so that a warp's store covers 4 rows of 128 bytes, not 32 of 16
-// (fp32 exponentials of 10 000 x 1000 logits of 100 products: 48 us in single rows of 16 bytes, NEW us so).
-__device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { return reinterpret_cast<uint4 *>(patch + r * 128 + ((c ^ (r & 7)) << 4)); }
+// 16-byte piece `c` of row `r` of a warp's patch: rows of 64 bytes whose pieces are exchanged so that both a piece of all rows and
+// whole rows are free of bank conflicts. Results go through it so that a warp's store covers 8 rows of 64 bytes, not 32 of 16.
+__device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { return reinterpret_cast<uint4 *>(patch + r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); }
 
 // Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end,
-// uint32_t (&acc)[N], uint8_t *patch) const`: called by the eight epilogue warps, lane by lane with N columns col .. of row
+// uint32_t (&acc)[N], uint8_t *patch) const`: called by the epilogue warps, lane by lane with N columns col .. of row
 // row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). All lanes
-// call. Epi::kStream: a tile is one chunk, and its columns come 32 at a time; else all BN / 2 of the warp at once.
-template <int CG, int BN, bool AMN, bool BMN, class Epi>
+// call. Epi::kStep: columns that it takes at a time (0: all of the warp's). kChunked: a tile may be of several chunks, and
+// finish gets all columns of the warp.
+template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s, const Epi epi)
 {
@@ -228,7 +239,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     extern __shared__ uint8_t smem_raw[];
     __shared__ alignas(8) uint64_t s_full[L::kStages], s_empty[L::kStages], s_done[2], s_free[2], s_drain;
     __shared__ uint32_t s_tmem;
-    __shared__ volatile uint32_t s_stop;
+    __shared__ volatile uint32_t s_stop, s_answer[2]; // (two answers: the thread that looks is less than two ahead)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -306,9 +317,14 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                     }
                 }
             }
-            if (!ok && rank == 0) // what is in flight still lands in this CTA's shared memory
-                for (uint32_t j = it > (uint32_t)L::kStages ? it - L::kStages : 0; j < it; ++j)
-                    bar_drain(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1);
+            // The products' arrivals at this CTA's barriers have to be there before it ends: its shared memory belongs to the next
+            // CTA on the SM then, and an arrival that comes late would count at that one's barrier. So the last use of every
+            // stage is waited for. (Stopped: the copies in flight, which complete at the leader's barriers.)
+            const uint32_t used = it < (uint32_t)L::kStages ? it : L::kStages;
+            for (uint32_t j = it - used; j < it; ++j) {
+                if (ok) ok = bar_wait(smem_u32(&s_empty[j % L::kStages]), (j / L::kStages) & 1, &s_stop);
+                else if (rank == 0) bar_drain(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1);
+            }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -342,36 +358,40 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                     commit<CG>(smem_u32(&s_done[acc]));
                 }
             }
+            // (and the epilogues' last arrivals, the other CTA's among them)
+            for (uint32_t j = n_chunk < 2 ? 0 : n_chunk - 2; ok && j < n_chunk; ++j) ok = bar_wait(smem_u32(&s_free[j & 1]), (j >> 1) & 1, &s_stop);
             if (s_stop) { // products in flight are waited for before tensor memory is given back
                 commit<CG>(smem_u32(&s_drain));
                 bar_drain(smem_u32(&s_drain), 0);
             }
         }
     } else {
-        constexpr int kN = BN / 2; // columns of a warp
+        constexpr int kN = BN * 4 / kEpiWarps; // columns of a warp
         // the lanes of tensor memory that a warp may read: 32 (its number in the CTA % 4) ..
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * kN);
+        const int quarter = warp & 3, part = (warp - 2) >> 2;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * kN);
         uint8_t *patch = smem_raw + (ring - smem_u32(smem_raw)) + L::kStages * L::kStageBytes + (warp - 2) * kPatchBytes;
         uint32_t n_chunk = 0;
         bool ok = true;
         for (int64_t t = first_tile; ok && t < tiles; t += stride) {
             const Tile tl = tile_of(s, t);
-            const int row0 = (tl.m * CG + (int)rank) * L::kBM + quarter * 32, col = tl.n * s.cols + half * kN;
+            const int row0 = (tl.m * CG + (int)rank) * L::kBM + quarter * 32, col = tl.n * s.cols + part * kN;
             const int end = min(s.n, (tl.n + 1) * s.cols); // the tile's columns end here
-            if constexpr (Epi::kStream) {
+            if constexpr (!kChunked) {
+                constexpr int kStep = Epi::kStep ? Epi::kStep : kN;
                 const uint32_t a = n_chunk & 1;
-                ok = lane == 0 ? bar_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop) : true;
-                ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, &s_answer[a], threadIdx.x == 64);
                 if (!ok) break;
                 ++n_chunk;
                 fence_after();
 #pragma unroll 1
-                for (int c = 0; c < kN && col + c < end; c += 32) {
-                    uint32_t r[32];
-                    load32(at + a * BN + c, r);
+                for (int c = 0; c < kN && col + c < end; c += kStep) {
+                    uint32_t r[kStep];
+#pragma unroll
+                    for (int j = 0; j < kStep; j += 32)
+                        if (j == 0 || col + c + j < end) load32(at + a * BN + c + j, *reinterpret_cast<uint32_t(*)[32]>(&r[j]));
                     wait_loads();
-                    epi.template finish<32>(s, tl, row0, lane, col + c, end, r, patch);
+                    epi.template finish<kStep>(s, tl, row0, lane, col + c, end, r, patch);
                 }
                 fence_before();
                 __syncwarp();
@@ -380,9 +400,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             uint32_t acc[kN];
             for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
                 const uint32_t a = n_chunk & 1;
-                // (one lane's verdict for the warp: the loads from tensor memory are the whole warp's)
-                ok = lane == 0 ? bar_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop) : true;
-                ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, &s_answer[a], threadIdx.x == 64);
                 if (!ok) break;
                 fence_after();
                 if (c0 == tl.first) {
