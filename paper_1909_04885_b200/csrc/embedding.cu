@@ -297,6 +297,7 @@ struct Sums {
     int accumulate;
     float *partial;       // [window][2][d]: of the run that came in, of the run that goes out
     int64_t sum_blocks;   // CTAs that sum; the others zero
+    int join_windows;     // windows per CTA of the joining kernel
 };
 
 template <typename T, int E>
@@ -323,8 +324,11 @@ template <int E> __device__ __forceinline__ void put_partial(const Sums &s, int6
     *reinterpret_cast<Vec<float, E> *>(s.partial + at * s.d + (int64_t)c * E) = o;
 }
 
+// Rows are fetched several at a time (16 bytes each), and enough CTAs have to fit on an SM for the zeroing ones to keep memory
+// busy: eight rows of 8 elements take 137 registers and leave room for one (16384 entries of 4096 bf16: 280 us, four rows and four
+// CTAs: 215; 131072 entries: 170 with three CTAs, 153 with four; 319488 entries of 64 fp32 the other way round, 132 with four and 116).
 template <typename T, int E>
-__global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__restrict__ grad, int64_t ld, T *__restrict__ table, int64_t ld_t,
+__global__ void __launch_bounds__(256, E == 8 ? 4 : 3) k_sum_by_id(const Sums s, const T *__restrict__ grad, int64_t ld, T *__restrict__ table, int64_t ld_t,
                                                    const ZeroJob zero)
 {
     if (blockIdx.x >= s.sum_blocks) return zero_block(zero, (int64_t)blockIdx.x - s.sum_blocks);
@@ -339,11 +343,11 @@ __global__ void __launch_bounds__(256) k_sum_by_id(const Sums s, const T *__rest
     bool from_before = e0 > 0 && s.keys[e0 - 1] == cur;
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[j] = 0.f;
-    constexpr int kAhead = 8;
+    constexpr int kAhead = E == 8 ? 4 : 8;
     for (int64_t e = e0; e < e1; e += kAhead) {
         // (windows begin at multiples of 8; the arrays have room behind the last entry)
-        const Vec<int32_t, 8> at = *reinterpret_cast<const Vec<int32_t, 8> *>(s.order + e);
-        Vec<int32_t, 8> keys = *reinterpret_cast<const Vec<int32_t, 8> *>(s.keys + e);
+        const Vec<int32_t, kAhead> at = *reinterpret_cast<const Vec<int32_t, kAhead> *>(s.order + e);
+        Vec<int32_t, kAhead> keys = *reinterpret_cast<const Vec<int32_t, kAhead> *>(s.keys + e);
         int32_t(&key)[kAhead] = keys.v;
         Vec<T, E> q[kAhead];
 #pragma unroll
@@ -392,12 +396,12 @@ __global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restric
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tpr = 1 << s.tpr_log;
     const int c_end = min(s.vecs, ((int)blockIdx.y + 1) * tpr), c_begin = (int)blockIdx.y * tpr;
-    const int64_t w0 = (int64_t)blockIdx.x * 8;
+    const int64_t w0 = (int64_t)blockIdx.x * s.join_windows;
     int64_t count = 0;
     {
         const int64_t w = w0 + warp;
         const int64_t e0 = w * s.window, e1 = e0 + s.window;
-        if (e1 < s.n) {
+        if (warp < s.join_windows && e1 < s.n) {
             const int32_t k = s.keys[e1], last = s.keys[e1 - 1], first = s.keys[e0], before = e0 > 0 ? s.keys[e0 - 1] : -1;
             if (last == k && k < s.rows && !(first == k && before == k)) {
                 // windows w + 1 .. the one with the run's last entry hold the rest
@@ -425,7 +429,7 @@ __global__ void __launch_bounds__(256) k_join_windows(const Sums s, T *__restric
     if (lane == 0) s_count[warp] = count;
     __syncthreads();
     const int groups = 256 >> s.tpr_log, g = threadIdx.x >> s.tpr_log, c = c_begin + (threadIdx.x & (tpr - 1));
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < s.join_windows; ++i) {
         count = s_count[i];
         if (count == 0) continue; // (the same for all threads)
         const int64_t w = w0 + i;
@@ -590,9 +594,11 @@ cudaError_t sum_by_id(Sums sm, const chicle_dense_t &g, const chicle_dense_t &t,
     sm.slabs = (int)ceil_div(sm.vecs, 1 << sm.tpr_log);
     sm.sum_blocks = ceil_div(sm.windows, 256 >> sm.tpr_log) * sm.slabs;
     k_sum_by_id<T, E><<<(unsigned)(sm.sum_blocks + zero.blocks()), 256, 0, s>>>(sm, (const T *)g.data, g.ld, (T *)t.data, t.ld, zero);
+    // (wide rows: a run's sums are the work of a CTA, and one CTA does them one behind the other)
+    sm.join_windows = sm.tpr_log == 8 ? 1 : 8;
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && sm.windows > 1) {
-        k_join_windows<T, E><<<dim3((unsigned)ceil_div(sm.windows, 8), (unsigned)sm.slabs), 256, 0, s>>>(sm, (T *)t.data, t.ld);
+        k_join_windows<T, E><<<dim3((unsigned)ceil_div(sm.windows, sm.join_windows), (unsigned)sm.slabs), 256, 0, s>>>(sm, (T *)t.data, t.ld);
         e = cudaGetLastError();
     }
     return e;

@@ -156,7 +156,7 @@ template <> __device__ __forceinline__ __half from_float<__half>(float v) { retu
 // Where a tile of a gradient goes. With splits: to `partial`, one plane per split. Else sum = (add ? *add : 0) + tile; to
 // `keep` (fp32, for the pieces that follow) or to `out`.
 template <typename OutT> struct GradEpilogue {
-    static constexpr int kStep = 32;
+    static constexpr int kStep = 32; // (not used where sums come in chunks)
     OutT *out;
     int64_t ld;
     float *partial;          // [split][m][n]
@@ -258,6 +258,20 @@ __global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ p
 
 // ---- small kernels -----------------------------------------------------------------------------------------
 
+// (top, sum) of one more block. Equal ones, infinite ones too, without a difference.
+__device__ __forceinline__ void join_into(float &top, float &sum, float2 o)
+{
+    const float m = fmaxf(top, o.x);
+    sum = (top == m ? sum : sum * exp2f((top - m) * kLog2e)) + (o.x == m ? o.y : o.y * exp2f((o.x - m) * kLog2e));
+    top = m;
+}
+
+// loss and lse of a row, relative to the largest logit: lse and the label's logit would lose the bits that they share.
+__device__ __forceinline__ float2 loss_of(float top, float sum, bool has, float label_logit)
+{
+    return has ? make_float2((top - label_logit) + logf(sum), top + logf(sum)) : make_float2(0.f, 0.f);
+}
+
 // Joins the blocks of classes of R rows per CTA; threads of one row run down its blocks, fixed order.
 template <int R>
 __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ stats, int blocks, int32_t n,
@@ -272,22 +286,14 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
     float top = -INFINITY, sum = 0.f;
     if (row < n) {
 #pragma unroll 4
-        for (int b = t; b < blocks; b += kT) {
-            const float2 o = stats[(int64_t)b * n + row];
-            const float m = fmaxf(top, o.x);
-            // (equal ones, infinite ones too, without a difference)
-            sum = (top == m ? sum : sum * exp2f((top - m) * kLog2e)) + (o.x == m ? o.y : o.y * exp2f((o.x - m) * kLog2e));
-            top = m;
-        }
+        for (int b = t; b < blocks; b += kT) join_into(top, sum, stats[(int64_t)b * n + row]);
     }
     s_top[t][r] = top;
     s_sum[t][r] = sum;
     __syncthreads();
     for (int w = kT / 2; w > 0; w >>= 1) {
         if (t < w) {
-            const float b = s_top[t + w][r], m = fmaxf(top, b), bs = s_sum[t + w][r];
-            sum = (top == m ? sum : sum * exp2f((top - m) * kLog2e)) + (b == m ? bs : bs * exp2f((b - m) * kLog2e));
-            top = m;
+            join_into(top, sum, make_float2(s_top[t + w][r], s_sum[t + w][r]));
             s_top[t][r] = top;
             s_sum[t][r] = sum;
         }
@@ -296,11 +302,10 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
     if (t == 0 && row < n) {
         const int32_t y = labels[row];
         const bool has = (uint32_t)y < (uint32_t)classes;
-        const float total = top + logf(sum);
+        const float2 l = loss_of(top, sum, has, has ? label_logit[row] : 0.f);
+        loss[row] = l.x;
+        lse[row] = l.y;
         if (norm) norm[row] = make_float2(top, 1.f / sum);
-        lse[row] = has ? total : 0.f;
-        // relative to the largest logit: lse and the label's logit would lose the bits that they share
-        loss[row] = has ? (top - label_logit[row]) + logf(sum) : 0.f;
         if (y >= classes && status) atomicOr(status, (uint32_t)ST_BAD_INDEX);
     }
 }
@@ -308,11 +313,12 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
 // Exponentials to P, kSteps times 8 classes of a row per thread: in place for 16-bit operands, from fp32 to two fp16 planes for
 // single precision. Bound by memory: 8192 x 131072 in 640 us, 6.7 TB/s (with one step 850; 10000 x 1000: one step 13 us, four
 // 26, most of whose threads have nothing to do).
-template <typename PT, bool kWide, int kSteps>
+// kJoin: a CTA has a whole row, and joins its blocks of classes itself (k_join_blocks): one launch less where launches count.
+template <typename PT, bool kWide, int kSteps, bool kJoin>
 __global__ void __launch_bounds__(256)
 k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, int32_t classes, const float2 *__restrict__ stats,
-                const float2 *__restrict__ norm, const float *__restrict__ loss, const int32_t *__restrict__ labels,
-                const float *__restrict__ weights, float scale, const float *__restrict__ lift, int block_log)
+                float2 *norm, float *loss, const int32_t *__restrict__ labels, const float *__restrict__ weights, float scale,
+                const float *__restrict__ lift, int block_log, int blocks, const float *__restrict__ label_logit, float *lse, uint32_t *status)
 {
     const int row = blockIdx.y;
     const int c0 = (blockIdx.x * kSteps * 256 + threadIdx.x) * 8;
@@ -336,7 +342,29 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
     }
     float g = weights ? weights[row] * scale : scale;
     if (lift) g *= *lift;
-    const float2 of = norm[row]; // relative to the largest logit: lse has lost the bits that the two share
+    float2 of;   // relative to the largest logit: lse has lost the bits that the two share
+    float of_label;
+    if constexpr (kJoin) {
+        // every warp joins the row's blocks for itself, 32 at a time
+        float top = -INFINITY, sum = 0.f;
+        for (int b = threadIdx.x & 31; b < blocks; b += 32) join_into(top, sum, stats[(int64_t)b * n + row]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            join_into(top, sum, make_float2(__shfl_xor_sync(0xffffffffu, top, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+        top = __shfl_sync(0xffffffffu, top, 0); // (the lanes' sums may differ in the last bit)
+        sum = __shfl_sync(0xffffffffu, sum, 0);
+        of = make_float2(top, 1.f / sum);
+        const float2 l = loss_of(top, sum, has, has ? label_logit[row] : 0.f);
+        of_label = l.x;
+        if (threadIdx.x == 0) {
+            loss[row] = l.x;
+            lse[row] = l.y;
+            if (y >= classes && status) atomicOr(status, (uint32_t)ST_BAD_INDEX);
+        }
+    } else {
+        of = norm[row];
+        of_label = loss[row];
+    }
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
         const int c = c0 + k * 2048;
@@ -358,7 +386,7 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
                 }
             }
             if (y >= c && y < c + 8) {
-                const float at = g * expm1f(-loss[row]);
+                const float at = g * expm1f(-of_label);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (y - c == j) v[j] = at;
@@ -380,44 +408,27 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
     }
 }
 
-// Rows in a layout that the bulk copies take (whole lines), single precision scaled and as two fp16 planes; rows without a label
-// become zeros where labels are given.
-template <typename T, typename P>
-__global__ void __launch_bounds__(256) k_pack(const T *__restrict__ src, int64_t ld, int64_t rows, int32_t d, P *__restrict__ dst,
-                                              int64_t pitch, int64_t plane, const int32_t *__restrict__ labels, int32_t classes,
-                                              const float *__restrict__ lift)
+// The power of two that takes a largest magnitude to [2^14, 2^15), and its inverse.
+__device__ __forceinline__ float2 scale_of(float top)
 {
-    const int per = (int)(pitch / 8);
-    const int64_t all = rows * per;
-    const float up = sizeof(T) == 4 ? *lift : 1.f;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per;
-        const int c = (int)(i - row * per) * 8;
-        const bool has = !labels || (uint32_t)labels[row] < (uint32_t)classes;
-        const T *from = src + row * ld + c;
-        alignas(16) T in[8];
-        if (has && c + 8 <= d && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
+    int e = 15;
+    if (top > 0.f) frexpf(top, &e); // top in [2^(e-1), 2^e)
+    e = max(-120, min(120, 15 - e));
+    return make_float2(ldexpf(1.f, e), ldexpf(1.f, -e));
+}
+
+// The largest of the CTA's 256 values.
+__device__ __forceinline__ float block_largest(float top)
+{
+    __shared__ float s[8];
 #pragma unroll
-            for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
-                reinterpret_cast<uint4 *>(in)[j] = reinterpret_cast<const uint4 *>(from)[j];
-        } else {
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = top;
+    __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) in[j] = has && c + j < d ? from[j] : from_float<T>(0.f);
-        }
-        if constexpr (sizeof(T) == 4) {
-            alignas(16) P hi[8], lo[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = in[j] * up;
-                hi[j] = from_float<P>(v);
-                lo[j] = from_float<P>(v - (float)hi[j]);
-            }
-            *reinterpret_cast<uint4 *>(dst + row * pitch + c) = *reinterpret_cast<const uint4 *>(hi);
-            *reinterpret_cast<uint4 *>(dst + plane + row * pitch + c) = *reinterpret_cast<const uint4 *>(lo);
-        } else {
-            *reinterpret_cast<uint4 *>(dst + row * pitch + c) = *reinterpret_cast<const uint4 *>(in);
-        }
-    }
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, s[i]);
+    return top;
 }
 
 // Largest finite magnitudes, one word per CTA: the first kMaxBlocks of X (rows with a label, where labels are given), the next of W.
@@ -427,7 +438,6 @@ __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, in
                                                  int32_t classes, const float *__restrict__ w, int64_t ld_w, int32_t d,
                                                  float *__restrict__ largest)
 {
-    __shared__ float s[8];
     const bool of_x = blockIdx.x < kMaxBlocks;
     const float *src = of_x ? x : w;
     const int64_t ld = of_x ? ld_x : ld_w, rows = of_x ? n : classes;
@@ -462,46 +472,82 @@ __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, in
             }
         }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
-        largest[blockIdx.x] = top;
-    }
+    top = block_largest(top);
+    if (threadIdx.x == 0) largest[blockIdx.x] = top;
 }
 
-// The scales. CTA 0: of P, from the weights; 1 and 2: of X and W, from the largest magnitudes (null: no such scales).
-__global__ void __launch_bounds__(512) k_scales(const float *__restrict__ weights, int64_t n, float scale, const float *__restrict__ largest,
-                                                float *__restrict__ scales)
+// One of the matrices that k_pack lays out. `lift`: words of Scales that its scale goes to (single precision).
+struct Packed {
+    const void *src;
+    int64_t ld, rows, plane;
+    void *dst;
+    const int32_t *labels; // rows without a label become zeros; or null
+    unsigned blocks;       // CTAs for it (0: it is used as it is)
+    int lift;
+};
+
+// Rows in a layout that the bulk copies take (whole lines), single precision scaled and as two fp16 planes. The first CTA of
+// a launch also finds the scale of P where there is one.
+template <typename T, typename P>
+__global__ void __launch_bounds__(256) k_pack(const Packed x, const Packed w, int32_t d, int64_t pitch, int32_t classes,
+                                              const float *__restrict__ largest, const float *__restrict__ weights, int64_t n, float scale,
+                                              float *__restrict__ scales)
 {
-    __shared__ float s[16];
-    float top = 0.f;
-    if (blockIdx.x == 0) {
+    const bool of_x = blockIdx.x < x.blocks;
+    const Packed &m = of_x ? x : w;
+    const unsigned block = of_x ? blockIdx.x : blockIdx.x - x.blocks;
+    if (scales && blockIdx.x == 0) {
+        float top = 0.f;
         if (weights) {
 #pragma unroll 4
-            for (int64_t i = threadIdx.x; i < n; i += 512) {
+            for (int64_t i = threadIdx.x; i < n; i += 256) {
                 const float v = fabsf(weights[i] * scale);
                 if (v < INFINITY) top = fmaxf(top, v);
             }
         } else {
             top = fabsf(scale);
         }
-    } else {
-        for (int i = threadIdx.x; i < kMaxBlocks; i += 512) top = fmaxf(top, largest[(blockIdx.x - 1) * kMaxBlocks + i]);
+        const float2 f = scale_of(block_largest(top));
+        if (threadIdx.x == 0) scales[kLift] = f.x, scales[kInvLift] = f.y;
     }
+    float up = 1.f;
+    if constexpr (sizeof(T) == 4) {
+        float top = 0.f;
+        for (int i = threadIdx.x; i < kMaxBlocks; i += 256) top = fmaxf(top, largest[(of_x ? 0 : kMaxBlocks) + i]);
+        const float2 f = scale_of(block_largest(top));
+        up = f.x;
+        if (block == 0 && threadIdx.x == 0) scales[m.lift] = f.x, scales[m.lift + 1] = f.y;
+    }
+    const int per = (int)(pitch / 8);
+    const int64_t all = m.rows * per;
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < all; i += (int64_t)m.blocks * 256) {
+        const int64_t row = i / per;
+        const int c = (int)(i - row * per) * 8;
+        const bool has = !m.labels || (uint32_t)m.labels[row] < (uint32_t)classes;
+        const T *from = static_cast<const T *>(m.src) + row * m.ld + c;
+        P *to = static_cast<P *>(m.dst) + row * pitch + c;
+        alignas(16) T in[8];
+        if (has && c + 8 <= d && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        int e = 15;
-        if (top > 0.f) frexpf(top, &e); // top in [2^(e-1), 2^e)
-        e = max(-120, min(120, 15 - e));
-        scales[2 * blockIdx.x] = ldexpf(1.f, e);
-        scales[2 * blockIdx.x + 1] = ldexpf(1.f, -e);
+            for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
+                reinterpret_cast<uint4 *>(in)[j] = reinterpret_cast<const uint4 *>(from)[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in[j] = has && c + j < d ? from[j] : from_float<T>(0.f);
+        }
+        if constexpr (sizeof(T) == 4) {
+            alignas(16) P hi[8], lo[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = in[j] * up;
+                hi[j] = from_float<P>(v);
+                lo[j] = from_float<P>(v - (float)hi[j]);
+            }
+            *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(hi);
+            *reinterpret_cast<uint4 *>(to + m.plane) = *reinterpret_cast<const uint4 *>(lo);
+        } else {
+            *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(in);
+        }
     }
 }
 
@@ -720,33 +766,24 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     return p;
 }
 
-cudaError_t pack(const chicle_dense_t &src, void *dst, const Plan &p, const int32_t *labels, const float *lift, cudaStream_t s)
+// Lays out what has to be, and finds the scales that these operands take (*scales: null where they take none).
+template <typename T, typename P>
+cudaError_t pack(const chicle_dense_t &X, const chicle_dense_t &W, const Plan &p, const int32_t *labels, const float *weights, float scale,
+                 uint8_t *ws, cudaStream_t s, bool grad, float **scales)
 {
-    const int64_t all = src.rows * (p.pitch_d / 8);
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(all, 256), kSms * 16);
-    const int64_t plane = src.rows * p.pitch_d;
-    if (src.type == CHICLE_F32)
-        k_pack<float, __half><<<grid, 256, 0, s>>>((const float *)src.data, src.ld, src.rows, (int32_t)p.d, (__half *)dst, p.pitch_d, plane, labels, (int32_t)p.v, lift);
-    else if (src.type == CHICLE_BF16)
-        k_pack<__nv_bfloat16, __nv_bfloat16><<<grid, 256, 0, s>>>((const __nv_bfloat16 *)src.data, src.ld, src.rows, (int32_t)p.d, (__nv_bfloat16 *)dst, p.pitch_d, plane, labels, (int32_t)p.v, nullptr);
-    else
-        k_pack<__half, __half><<<grid, 256, 0, s>>>((const __half *)src.data, src.ld, src.rows, (int32_t)p.d, (__half *)dst, p.pitch_d, plane, labels, (int32_t)p.v, nullptr);
-    return cudaGetLastError();
-}
-
-// The scales that these operands take; null where they take none.
-cudaError_t find_scales(const chicle_dense_t &X, const chicle_dense_t &W, const Plan &p, const int32_t *labels, const float *weights,
-                        float scale, uint8_t *ws, cudaStream_t s, float **scales)
-{
-    *scales = nullptr;
-    if (!p.half) return cudaSuccess;
-    *scales = reinterpret_cast<float *>(ws + p.scales);
+    *scales = p.wide || (p.half && grad) ? reinterpret_cast<float *>(ws + p.scales) : nullptr;
     float *largest = nullptr;
     if (p.wide) {
         largest = reinterpret_cast<float *>(ws + p.largest);
         k_largest<<<2 * kMaxBlocks, 256, 0, s>>>((const float *)X.data, X.ld, p.n, labels, (int32_t)p.v, (const float *)W.data, W.ld, (int32_t)p.d, largest);
     }
-    k_scales<<<p.wide ? 3 : 1, 512, 0, s>>>(weights, p.n, scale, largest, *scales);
+    auto part = [&](const chicle_dense_t &m, bool is_packed, size_t at, const int32_t *rows_with, int lift) {
+        const int64_t blocks = is_packed ? std::min<int64_t>(ceil_div(m.rows * (p.pitch_d / 8), 256), kSms * 16) : 0;
+        return Packed{m.data, m.ld, m.rows, m.rows * p.pitch_d, ws + at, rows_with, (unsigned)blocks, lift};
+    };
+    const Packed x = part(X, p.pack_x, p.x, labels, kLiftX), w = part(W, p.pack_w, p.w, nullptr, kLiftW);
+    if (x.blocks + w.blocks)
+        k_pack<T, P><<<x.blocks + w.blocks, 256, 0, s>>>(x, w, (int32_t)p.d, p.pitch_d, (int32_t)p.v, largest, weights, p.n, scale, *scales);
     return cudaGetLastError();
 }
 
@@ -816,9 +853,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
 {
     constexpr bool kWide = sizeof(T) == 4;
     float *scales;
-    cudaError_t e = find_scales(X, W, p, labels, weights, scale, ws, stream, &scales);
-    if (e == cudaSuccess) e = pack(X, ws + p.x, p, labels, scales + kLiftX, stream);
-    if (e == cudaSuccess && p.pack_w) e = pack(W, ws + p.w, p, nullptr, scales + kLiftW, stream);
+    cudaError_t e = pack<T, PT>(X, W, p, labels, weights, scale, ws, stream, true, &scales);
     const Operand w = operand_of(W, ws + p.w, p.pack_w, p);
     for (int64_t r0 = 0; e == cudaSuccess && r0 < p.n; r0 += p.piece) {
         const int64_t rows = std::min(p.piece, p.n - r0);
@@ -832,17 +867,22 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         PT *prob = reinterpret_cast<PT *>(ws + p.p);
         const LogitsEpilogue<StoreT> le{labels + r0, stats, label_logit, store, p.ld_v, kWide ? scales : nullptr};
         e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), status), p.cols, le, stream);
-        if (e == cudaSuccess) e = join_blocks(p, stats, rows, labels + r0, label_logit, loss + r0, lse + r0, norm, status, stream);
+        // a CTA of the elementwise pass has a whole row; it takes longer so, which shows where the rows take several turns (10000
+        // rows: 4 us more than the launch)
+        const bool joins = p.v <= 2048 && rows <= 8 * kSms;
+        if (e == cudaSuccess && !joins) e = join_blocks(p, stats, rows, labels + r0, label_logit, loss + r0, lse + r0, norm, status, stream);
         if (e != cudaSuccess) break;
         Operand q;
         q.data = prob;
         q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.planes;
         const int steps = p.v >= 8192 ? 4 : 1;
-        auto *probabilities = steps == 4 ? k_probabilities<PT, kWide, 4> : k_probabilities<PT, kWide, 1>;
+        auto *probabilities = steps == 4 ? k_probabilities<PT, kWide, 4, false>
+                              : joins  ? k_probabilities<PT, kWide, 1, true>
+                                       : k_probabilities<PT, kWide, 1, false>;
         for (int64_t y = 0; y < rows; y += 65535)
             probabilities<<<dim3((unsigned)ceil_div(p.v, 2048 * steps), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
                 labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr,
-                __builtin_ctz(tile_columns(p.v) / p.parts));
+                __builtin_ctz(tile_columns(p.v) / p.parts), (int)blocks_of(p.v, p.cols, p.parts), label_logit + y, lse + r0 + y, status);
         if ((e = cudaGetLastError()) != cudaSuccess) break;
         const float *back = scales ? scales + kInvLift : nullptr;
         float *partial = reinterpret_cast<float *>(ws + p.partial);
@@ -933,10 +973,10 @@ extern "C" chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, co
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     uint8_t *ws = static_cast<uint8_t *>(dev_workspace);
     float *scales = nullptr;
-    cudaError_t e = p.wide ? find_scales(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, &scales) : cudaSuccess;
     // (rows without a label are left out of the scale, so they have to be zeros)
-    if (e == cudaSuccess && p.pack_x) e = pack(*X, ws + p.x, p, dev_labels, scales + kLiftX, s);
-    if (e == cudaSuccess && p.pack_w) e = pack(*W, ws + p.w, p, nullptr, scales + kLiftW, s);
+    cudaError_t e = p.wide ? pack<float, __half>(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, false, &scales)
+                    : p.half ? pack<__half, __half>(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, false, &scales)
+                             : pack<__nv_bfloat16, __nv_bfloat16>(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, false, &scales);
     float2 *stats = reinterpret_cast<float2 *>(ws + p.stats);
     float *label_logit = reinterpret_cast<float *>(ws + p.label_logit);
     const LogitsEpilogue<NoStore> le{dev_labels, stats, label_logit, nullptr, 0, scales};
