@@ -319,8 +319,9 @@ typedef struct {
 /* Softmax cross entropy of the linear map X W^T to W->rows classes: with l_iv = x_i . w_v,
  *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, label_i},
  * one float per row each. A row whose label is negative has no label: its loss and lse are 0, and what it holds has no
- * effect. X and W have one type; products are summed in fp32 (fp32 operands: to fp32 accuracy), and the logits are not kept.
- * Values that are not finite give results that are not finite. chicle_softmax_workspace gives the bytes of workspace
+ * effect. X and W have one type; products are summed in fp32, and the logits are not kept. fp32 elements are
+ * taken to 2^-22 of themselves, or 2^-39 of the largest magnitude in their matrix where that is more (rows without a label left
+ * out): as exact as a sum in fp32, unless magnitudes within a matrix are further apart than 2^17. Values that are not finite give results that are not finite. chicle_softmax_workspace gives the bytes of workspace
  * (256-byte aligned) for the same descriptions (host only, no device is touched). */
 chicle_status_t chicle_softmax_workspace(const chicle_dense_t *X, const chicle_dense_t *W, int gradients, size_t *host_bytes);
 chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
@@ -362,7 +363,8 @@ typedef struct {
 /* *dev_norm = the 2-norm of all elements of all tensors (squares summed in fp64 in a fixed order), and
  * out = in * min(1, max_norm / (norm + 1e-6)) for each of them. A norm that is not finite leaves the elements as they are
  * (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors is a host array, read
- * during the call; in and out are the same or do not overlap. Workspace: CHICLE_CLIP_WORKSPACE bytes, 256-byte aligned. */
+ * during the call. An out is the tensor's own in or overlaps neither any in nor another out (a tensor listed twice with a result
+ * is refused; without results it counts twice). Workspace: CHICLE_CLIP_WORKSPACE bytes, 256-byte aligned. */
 #define CHICLE_CLIP_WORKSPACE 16384
 chicle_status_t chicle_clip_gradients(int device, void *cuda_stream, int64_t count, const chicle_tensor_t *host_tensors, float max_norm,
                                       float *dev_norm, void *dev_workspace, size_t workspace_bytes, char *host_errbuf,

@@ -513,8 +513,12 @@ def _operator(fn):
         if stream is None:
             return fn(*args, **kw)
         import torch
-        first = args[0] if args else next(iter(kw.values()))
-        first = first if hasattr(first, "device") else list(first)[0]
+        first = args[0]
+        if not isinstance(first, torch.Tensor):  # several: an iterator is used up here
+            args = (list(first),) + args[1:]
+            if not args[0]:
+                return fn(*args, **kw)
+            first = args[0][0]
         with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=first.device)):
             return fn(*args, **kw)
     return call

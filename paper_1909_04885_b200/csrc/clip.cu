@@ -10,6 +10,7 @@
 // when squared: those are squared in fp64.
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "operators.cuh"
 
@@ -172,6 +173,33 @@ __global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table<M> 
     }
 }
 
+// Whether elements that one tensor's result goes to are read or written for another one too (the same tensor listed twice, say):
+// CTAs would race on them.
+bool results_overlap(const chicle_tensor_t *x, int64_t count)
+{
+    struct Span {
+        uintptr_t from, to;
+        bool written;
+    };
+    std::vector<Span> spans;
+    spans.reserve((size_t)count * 2);
+    for (int64_t i = 0; i < count; ++i) {
+        if (x[i].n == 0) continue;
+        const uintptr_t bytes = (uintptr_t)x[i].n * (x[i].type == CHICLE_F32 ? 4 : 2);
+        const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].in), b = reinterpret_cast<uintptr_t>(x[i].out);
+        if (b) spans.push_back({b, b + bytes, true});
+        if (a != b) spans.push_back({a, a + bytes, false});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span &p, const Span &q) { return p.from < q.from; });
+    uintptr_t any = 0, written = 0; // where the spans so far end
+    for (const Span &s : spans) {
+        if (s.from < (s.written ? any : written)) return true;
+        any = std::max(any, s.to);
+        if (s.written) written = std::max(written, s.to);
+    }
+    return false;
+}
+
 struct Call {
     const chicle_tensor_t *tensors;
     int64_t count;
@@ -244,8 +272,12 @@ extern "C" chicle_status_t chicle_clip_gradients(int device, void *cuda_stream, 
         if (x.n > 0 && !x.in) return err(CHICLE_ERR_INVALID_ARG, "a tensor's data is NULL");
         const uintptr_t es = x.type == CHICLE_F32 ? 4 : 2, a = reinterpret_cast<uintptr_t>(x.in), b = reinterpret_cast<uintptr_t>(x.out);
         if (a % es || b % es) return err(CHICLE_ERR_INVALID_ARG, "data is not aligned to its element type");
-        if (b && a != b && a < b + (uintptr_t)x.n * es && b < a + (uintptr_t)x.n * es)
-            return err(CHICLE_ERR_INVALID_ARG, "in and out must be the same or not overlap");
+    }
+    try {
+        if (results_overlap(host_tensors, count))
+            return err(CHICLE_ERR_INVALID_ARG, "a tensor's out must be its in, or overlap neither an in nor another out (is a tensor listed twice?)");
+    } catch (...) {
+        return err(CHICLE_ERR_OOM, "host allocation failed");
     }
     const DeviceGuard guard(device);
     if (!guard.ok()) return err(CHICLE_ERR_CUDA, guard.message());

@@ -4,16 +4,20 @@
 //   l_iv = x_i . w_v        lse_i = log sum_v exp(l_iv)        loss_i = lse_i - l_{i, y_i}
 //   p_iv = g_i (exp(l_iv - lse_i) - [v = y_i])                 dX = P W,  dW = P^T X
 //
-// The logits are never held as a whole. The loss alone keeps, per row and block of classes (a warp's columns of a tile), the largest logit and the sum
-// of exponentials relative to it; a second kernel joins them. For the gradients the rows are taken in pieces of about two
-// gigabytes of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the largest of the row in the
-// block) as fp16, scaled by 2^15 so that what is 2^-29 of the tile's largest still has all its bits; an elementwise
-// pass turns the piece into P in place, and two products take dX and the piece's share of dW from it. So the
-// logits are computed once: 6 n V d operations, against 8 where they are computed again for the gradient, for 6 bytes of traffic
-// per logit (at d = 4096 a third of the products' time against a twentieth).
+// The logits are never held as a whole. The loss alone keeps, per row and block of classes (a warp's columns of a tile), the
+// largest logit and the sum of exponentials relative to it; a second kernel joins them. For the gradients the rows are
+// taken in pieces of about two gigabytes of 16-bit values: the product's epilogue writes exp(l - m) of its tile (m: the
+// largest of the row in the block) as fp16, an elementwise pass turns the piece into P in place, and two products
+// take dX and the piece's share of dW from it. So the logits are computed once: 6 n V d operations, against 8 where they
+// are computed again for the gradient, for 6 bytes of traffic per logit (at d = 4096 a third of the products' time against a
+// twentieth).
 //
-// Rounding: logits, sums and gradients in fp32; P is rounded once to the operands' type (fp16: scaled so that the largest
-// weight comes to 2^14 and more; single precision: to two fp16 planes, tensor_core.cuh), and the entry of the label comes from expm1(-loss), not from a difference.
+// Rounding: logits, sums and gradients in fp32. The exponentials are held times 2^15, so that 2^-29 of the block's
+// largest still has all its bits (single precision: in fp32). P is rounded once to the operands' type (fp16: scaled so that the
+// largest weight comes to 2^14 and more; single precision: to two fp16 planes, tensor_core.cuh), and the entry of the label
+// comes from expm1(-loss), not from a difference. That entry's rounding is most of what a gradient is off by beside the
+// rounding of the result: together 1.41 times the result's alone, more where one row decides. (Exponentials in 16 bits with half
+// of fp16's step, no sign bit, changed nothing.)
 #include <algorithm>
 #include <cmath>
 
@@ -57,7 +61,7 @@ enum { kLift, kInvLift, kLiftX, kInvX, kLiftW, kInvW, kScales };
 // ---- epilogues ---------------------------------------------------------------------------------------------
 
 // Reduces a tile of logits to (largest, sum of exponentials) per row and N classes, keeps the label's logit, and
-// writes the exponentials for the gradients: StoreT void (loss alone), half, or float (single precision).
+// writes the exponentials for the gradients: StoreT NoStore (loss alone), half, or float (single precision).
 template <typename StoreT> struct LogitsEpilogue {
     static constexpr int kStep = 0;
     const int32_t *labels; // rows of this piece
@@ -691,6 +695,7 @@ int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs)
 }
 
 constexpr int64_t kPieceBytes = (int64_t)1 << 31;
+constexpr int64_t kStatBytes = (int64_t)1 << 30; // the loss alone: pairs of (largest, sum), for so many bytes of rows at a time
 
 struct Plan {
     bool wide, half; // single precision; operands in fp16 (else bf16)
@@ -739,6 +744,9 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
         rows = std::max(rows, std::min<int64_t>(2048, 4 * kPieceBytes / (p.ld_v * logit_bytes(p.wide))));
         rows = std::max<int64_t>(rows, 256);
         if (rows < p.n) p.piece = ceil_div(ceil_div(p.n, ceil_div(p.n, rows)), 256) * 256;
+    } else {
+        const int64_t rows = std::max<int64_t>(4096, kStatBytes / (blocks_of(p.v, p.cols, p.parts) * (int64_t)sizeof(float2)) / 256 * 256);
+        p.piece = std::min(p.n, rows);
     }
     if (p.pack_x) p.x = take((size_t)p.planes * p.n * p.pitch_d * 2);
     if (p.pack_w) p.w = take((size_t)p.planes * p.v * p.pitch_d * 2);
@@ -979,11 +987,16 @@ extern "C" chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, co
                              : pack<__nv_bfloat16, __nv_bfloat16>(*X, *W, p, dev_labels, nullptr, 1.f, ws, s, false, &scales);
     float2 *stats = reinterpret_cast<float2 *>(ws + p.stats);
     float *label_logit = reinterpret_cast<float *>(ws + p.label_logit);
-    const LogitsEpilogue<NoStore> le{dev_labels, stats, label_logit, nullptr, 0, scales};
-    if (e == cudaSuccess)
-        e = run_logits(operand_of(*X, ws + p.x, p.pack_x, p), operand_of(*W, ws + p.w, p.pack_w, p),
-                                                 shape_of(p, p.n, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), dev_status), p.cols, le, s);
-    if (e == cudaSuccess) e = join_blocks(p, stats, p.n, dev_labels, label_logit, dev_loss, dev_lse, nullptr, dev_status, s);
+    const Operand w = operand_of(*W, ws + p.w, p.pack_w, p);
+    for (int64_t r0 = 0; e == cudaSuccess && r0 < p.n; r0 += p.piece) {
+        const int64_t rows = std::min(p.piece, p.n - r0);
+        Operand x = operand_of(*X, ws + p.x, p.pack_x, p);
+        x.data = static_cast<const uint16_t *>(x.data) + r0 * x.pitch; // (16-bit elements, planes too)
+        x.rows = rows;
+        const LogitsEpilogue<NoStore> le{dev_labels + r0, stats, label_logit, nullptr, 0, scales};
+        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(rows)), dev_status), p.cols, le, s);
+        if (e == cudaSuccess) e = join_blocks(p, stats, rows, dev_labels + r0, label_logit, dev_loss + r0, dev_lse + r0, nullptr, dev_status, s);
+    }
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
 }
 

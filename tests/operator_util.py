@@ -40,13 +40,13 @@ def softmax_reference(x, w, labels, weights=None, scale=1.0):
     # lse and loss: the logits' error, exponentials, their sum and the logarithm, the largest logit's rounding when added
     off_lse = torch.where(has, off + (v / 16 + 32) * STEP + 2 * STEP * (lse.abs() + logits.abs().amax(1)), zero)
     off_loss = torch.where(has, 2 * off + (v / 16 + 32) * STEP + 4 * STEP * (loss.abs() + logits.abs().amax(1)), zero)
-    # an entry of P: of exp(logit - lse) the two errors and the exponentials' (16 steps); its storage in between (fp16 2^-12,
+    # an entry of P: of exp(logit - lse) the two errors and the exponentials' (16 steps); its storage in between (fp16, 2^-11,
     # and of small ones 2^-40 of the largest) and its rounding; fp16 and its planes: of the lifted value, which may be subnormal
     gs = g.abs()[:, None]
     rel = (2 * (off + off_lse) + 16 * STEP)[:, None]
     off_p = soft * gs * rel + p.abs() * (4 * STEP if single else HALF[dt])
     if not single:
-        off_p = off_p + soft * gs * 2.0 ** -12 + gs * 2.0 ** -40
+        off_p = off_p + soft * gs * 2.0 ** -11 + gs * 2.0 ** -40
     if dt != torch.bfloat16:
         off_p = off_p + float(gs.max()) * 2.0 ** -37
     Wa, Xa = W.abs(), X.abs()

@@ -109,12 +109,29 @@ def test_norm_alone_and_captured(ops):
     assert all(torch.equal(x, y) for x, y in zip(out, eager))
 
 
+def test_neighbours_and_streams(ops):
+    """Pieces of one buffer next to each other, given as an iterator, on another stream; the same tensor twice for its norm alone."""
+    flat = torch.randn(20000, device="cuda")
+    want = [flat.clone() for _ in range(2)]
+    n = float(ops.clip_gradients([want[0][:7], want[0][7:]], 1.0))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    m = ops.clip_gradients((flat[a:b] for a, b in ((0, 7), (7, 20000))), 1.0, stream=side.cuda_stream)
+    side.synchronize()
+    assert float(m) == n and torch.equal(flat, want[0])
+    # (in place, and the pieces in the other order: the same sum in another order of its parts)
+    ops.clip_gradients([want[1][7:], want[1][:7]], 1.0)
+    assert torch.allclose(want[1], want[0], rtol=4 * NORM, atol=0)
+
+
 def test_refusals(ops):
     t = torch.randn(8, 8, device="cuda")
     for f in (lambda: ops.clip_gradients([], 1.0), lambda: ops.clip_gradients([t], -1.0), lambda: ops.clip_gradients([t], float("nan")),
               lambda: ops.clip_gradients([t.T[1:]], 1.0), lambda: ops.clip_gradients([t.cpu()], 1.0), lambda: ops.clip_gradients([t.double()], 1.0),
               lambda: ops.clip_gradients([t], 1.0, out=[t.half()]), lambda: ops.clip_gradients([t], 1.0, out=[]),
-              lambda: ops.clip_gradients([t[:4]], 1.0, out=[t[1:5]])):
+              lambda: ops.clip_gradients([t[:4]], 1.0, out=[t[1:5]]), lambda: ops.clip_gradients([t, t], 1.0),
+              lambda: ops.clip_gradients([t[:5], t[4:]], 1.0), lambda: ops.clip_gradients([t[:2], t[2:4]], 1.0, out=[t[4:6], t[4:6]]),
+              lambda: ops.clip_gradients([t[:2], t[2:4]], 1.0, out=[t[4:6], t[1:3]])):
         with pytest.raises((ValueError, ops.ChicleError)):
             f()
 

@@ -181,6 +181,19 @@ def test_several_pieces(ops, dtype):
         check(t, want[name], name)
 
 
+def test_loss_of_many_rows(ops):
+    """So many rows that the loss takes them in pieces: rows around the pieces' ends."""
+    n, v, d = 180000, 100000, 16
+    x, w, labels, _ = inputs(n, v, d, torch.bfloat16, without=0.1)
+    loss, lse = ops.softmax_loss(x, w, labels)
+    piece = (1 << 30) // (8 * 2 * -(-v // 256)) // 256 * 256  # pairs of floats, two per tile of 256 classes
+    assert 4096 < piece < n
+    rows = torch.cat([torch.arange(0, 60), torch.arange(piece - 60, piece + 60), torch.arange(n - 60, n)]).cuda()
+    want = softmax_reference(x[rows], w, labels[rows])
+    check(loss[rows], want["loss"], "loss")
+    check(lse[rows], want["lse"], "lse")
+
+
 def test_refusals(ops):
     x, w, labels, weights = inputs(8, 6, 16, torch.float32)
     bad = [
@@ -196,6 +209,7 @@ def test_refusals(ops):
         lambda: ops.softmax_loss_grad(x, w, labels, weights=weights[:3]),
         lambda: ops.softmax_loss_grad(x, w, labels, scale=float("nan")),
         lambda: ops.softmax_loss_grad(x, w, labels, weights=weights.double()),
+        lambda: ops.softmax_loss(x, w, labels, status=torch.zeros(2, dtype=torch.int32, device="cuda")),
     ]
     for f in bad:
         with pytest.raises((ValueError, ops.ChicleError)):
