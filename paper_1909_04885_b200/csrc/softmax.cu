@@ -179,6 +179,38 @@ template <typename OutT> struct GradEpilogue {
         const uint32_t zeros = __ballot_sync(0xffffffffu, labels && row0 + lane < s.m && (uint32_t)labels[row0 + lane] >= (uint32_t)classes);
         float *dst32 = partial ? partial + (int64_t)tl.split * s.m * s.n : keep;
         const float *src = partial ? nullptr : add;
+        if constexpr (sizeof(OutT) == 2 && N == 32) {
+            // straight to the result: rounded first, so that a warp's store covers 8 rows of 64 bytes
+            if (!whole && !src && ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * 2)) & 15) == 0) {
+                const bool zero = (zeros >> lane) & 1u;
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    alignas(16) OutT q[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) q[j] = from_float<OutT>(zero ? 0.f : __uint_as_float(r[8 * c + j]) * f);
+                    *tc::patch_at(patch, lane, c) = *reinterpret_cast<const uint4 *>(q);
+                }
+                __syncwarp();
+                const int col = c0 + 8 * (lane & 3);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int rr = 8 * i + (lane >> 2), row = row0 + rr;
+                    if (row >= s.m || col >= end) continue;
+                    alignas(16) OutT q[8];
+                    *reinterpret_cast<uint4 *>(q) = *tc::patch_at(patch, rr, lane & 3);
+                    OutT *dst = out + (int64_t)row * ld + col;
+                    if (col + 8 <= end) {
+                        *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(q);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (col + j < end) dst[j] = q[j];
+                    }
+                }
+                return;
+            }
+        }
         const bool quads = (s.n & 3) == 0; // fp32 rows of n: 16-byte pieces
         const bool quads_out = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * sizeof(OutT))) & (4 * sizeof(OutT) - 1)) == 0;
 #pragma unroll
@@ -318,7 +350,8 @@ __global__ void __launch_bounds__(512) k_join_blocks(const float2 *__restrict__ 
 // single precision. Bound by memory: 8192 x 131072 in 640 us, 6.7 TB/s (with one step 850; 10000 x 1000: one step 13 us, four
 // 26, most of whose threads have nothing to do).
 // kJoin: a CTA has a whole row, and joins its blocks of classes itself (k_join_blocks): one launch less where launches count.
-template <typename PT, bool kWide, int kSteps, bool kJoin>
+// kPlanes: of P.
+template <typename PT, bool kWide, int kPlanes, int kSteps, bool kJoin>
 __global__ void __launch_bounds__(256)
 k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, int32_t classes, const float2 *__restrict__ stats,
                 float2 *norm, float *loss, const int32_t *__restrict__ labels, const float *__restrict__ weights, float scale,
@@ -401,7 +434,7 @@ k_probabilities(const void *store, PT *p, int64_t ld, int64_t plane, int32_t n, 
         }
         alignas(16) PT q[8];
 #pragma unroll
-        for (int w = 0; w < (kWide ? 2 : 1); ++w) {
+        for (int w = 0; w < kPlanes; ++w) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 q[j] = from_float<PT>(v[j]);
@@ -695,11 +728,13 @@ int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs)
 }
 
 constexpr int64_t kPieceBytes = (int64_t)1 << 31;
+constexpr int64_t kFewRows = 32;
 constexpr int64_t kStatBytes = (int64_t)1 << 30; // the loss alone: pairs of (largest, sum), for so many bytes of rows at a time
 
 struct Plan {
     bool wide, half; // single precision; operands in fp16 (else bf16)
-    int planes, pairs;
+    int planes, pairs;                  // of the operands
+    int p_planes, grad_pairs;           // of P, and products of planes of the gradients
     int64_t n, v, d;
     bool pack_x, pack_w;
     int64_t pitch_d, ld_v;
@@ -718,6 +753,10 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     p.half = X.type != CHICLE_BF16;
     p.planes = p.wide ? 2 : 1;
     p.pairs = p.wide ? 3 : 1;
+    // Few rows: P in two planes. One row's gradients hang on the rounding of one or a few entries of P (n = 1: twice what the
+    // rounding of the result costs), and the products of few rows wait for W and dW anyway.
+    p.p_planes = p.wide || X.rows <= kFewRows ? 2 : 1;
+    p.grad_pairs = p.wide ? 3 : p.p_planes;
     p.n = X.rows, p.v = W.rows, p.d = X.cols;
     p.pack_x = grad || !takes_bulk(X);
     p.pack_w = !takes_bulk(W);
@@ -728,7 +767,7 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     // takes on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 512:
     // 7e-7, 256: 4e-7); all of them where a gradient is rounded to 16 bits in the end.
     p.logit_chunk = (p.wide ? 512 : 1024) / tc::kBK;
-    p.grad_chunk = p.wide ? 512 / tc::kBK : INT32_MAX / 2;
+    p.grad_chunk = (p.wide ? 512 : 1024) / tc::kBK; // (16 bits: one accumulator, what is fetched again is in L2 still)
     p.parts = tc::kEpiWarps / 4;
     p.cols = logit_columns(p.n, p.v, p.parts, grad);
     size_t at = 0;
@@ -757,12 +796,15 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
         if (p.wide) {
             p.store = take((size_t)p.piece * p.ld_v * 4);
             p.p = take((size_t)2 * p.piece * p.ld_v * 2);
+        } else if (p.p_planes == 2) {
+            p.store = take((size_t)p.piece * p.ld_v * 2);
+            p.p = take((size_t)2 * p.piece * p.ld_v * 2);
         } else {
             p.store = p.p = take((size_t)p.piece * p.ld_v * 2);
         }
         if (p.piece < p.n) p.acc = take((size_t)p.v * p.d * 4);
-        p.splits_x = plan_splits(p.piece, p.d, ceil_div(p.v, tc::kBK), p.pairs);
-        p.splits_w = plan_splits(p.v, p.d, ceil_div(p.piece, tc::kBK), p.pairs);
+        p.splits_x = plan_splits(p.piece, p.d, ceil_div(p.v, tc::kBK), p.grad_pairs);
+        p.splits_w = plan_splits(p.v, p.d, ceil_div(p.piece, tc::kBK), p.grad_pairs);
         size_t part = 0;
         if (p.splits_x > 1) part = (size_t)p.splits_x * p.piece * p.d * 4;
         if (p.splits_w > 1) part = std::max(part, (size_t)p.splits_w * p.v * p.d * 4);
@@ -807,12 +849,12 @@ Operand operand_of(const chicle_dense_t &src, const void *packed, bool is_packed
     return o;
 }
 
-tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int chunk, int splits, int group, uint32_t *status)
+tc::Shape shape_of(const Plan &p, int64_t m, int64_t n, int64_t k, int pairs, int chunk, int splits, int group, uint32_t *status)
 {
     tc::Shape s{};
     s.m = (int32_t)m, s.n = (int32_t)n;
     s.k_steps = (int32_t)ceil_div(k, tc::kBK);
-    s.pairs = p.pairs;
+    s.pairs = pairs;
     s.chunk = chunk;
     s.splits = splits;
     s.group = group;
@@ -874,7 +916,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         StoreT *store = reinterpret_cast<StoreT *>(ws + p.store);
         PT *prob = reinterpret_cast<PT *>(ws + p.p);
         const LogitsEpilogue<StoreT> le{labels + r0, stats, label_logit, store, p.ld_v, kWide ? scales : nullptr};
-        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), status), p.cols, le, stream);
+        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.pairs, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(p.n)), status), p.cols, le, stream);
         // a CTA of the elementwise pass has a whole row; it takes longer so, which shows where the rows take several turns (10000
         // rows: 4 us more than the launch)
         const bool joins = p.v <= 2048 && rows <= 8 * kSms;
@@ -882,11 +924,15 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         if (e != cudaSuccess) break;
         Operand q;
         q.data = prob;
-        q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.planes;
+        q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.p_planes;
         const int steps = p.v >= 8192 ? 4 : 1;
-        auto *probabilities = steps == 4 ? k_probabilities<PT, kWide, 4, false>
-                              : joins  ? k_probabilities<PT, kWide, 1, true>
-                                       : k_probabilities<PT, kWide, 1, false>;
+        constexpr int kMany = kWide ? 2 : 1; // planes of P where rows are many
+        auto *probabilities = p.p_planes != kMany ? (steps == 4 ? k_probabilities<PT, kWide, 2, 4, false>
+                                                     : joins    ? k_probabilities<PT, kWide, 2, 1, true>
+                                                                : k_probabilities<PT, kWide, 2, 1, false>)
+                              : steps == 4        ? k_probabilities<PT, kWide, kMany, 4, false>
+                              : joins             ? k_probabilities<PT, kWide, kMany, 1, true>
+                                                  : k_probabilities<PT, kWide, kMany, 1, false>;
         for (int64_t y = 0; y < rows; y += 65535)
             probabilities<<<dim3((unsigned)ceil_div(p.v, 2048 * steps), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
                 labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr,
@@ -896,7 +942,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         float *partial = reinterpret_cast<float *>(ws + p.partial);
         GradEpilogue<T> ex{static_cast<T *>(dX.data) + r0 * dX.ld, dX.ld, p.splits_x > 1 ? partial : nullptr, nullptr, nullptr, back,
                            kWide ? scales + kInvW : nullptr, labels + r0, (int32_t)p.v};
-        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, p.grad_chunk, p.splits_x, 8, status), ex, stream);
+        e = gradient<T>(p, q, w, true, shape_of(p, rows, p.d, p.v, p.grad_pairs, p.grad_chunk, p.splits_x, 8, status), ex, stream);
         if (e != cudaSuccess) break;
         // dW over the pieces: the sums stay in fp32 until the last
         const bool first = r0 == 0, last = r0 + rows >= p.n;
@@ -906,7 +952,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         if (!last) ew.keep = acc;
         const int splits = (int)std::min<int64_t>(p.splits_w, ceil_div(rows, tc::kBK));
         if (splits > 1) ew.partial = partial;
-        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, p.grad_chunk, splits, 8, status), ew, stream);
+        e = gradient<T>(p, q, x, false, shape_of(p, p.v, p.d, rows, p.grad_pairs, p.grad_chunk, splits, 8, status), ew, stream);
     }
     return e;
 }
@@ -994,7 +1040,7 @@ extern "C" chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, co
         x.data = static_cast<const uint16_t *>(x.data) + r0 * x.pitch; // (16-bit elements, planes too)
         x.rows = rows;
         const LogitsEpilogue<NoStore> le{dev_labels + r0, stats, label_logit, nullptr, 0, scales};
-        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(rows)), dev_status), p.cols, le, s);
+        e = run_logits(x, w, shape_of(p, rows, p.v, p.d, p.pairs, p.logit_chunk, 1, group_of(p.d, p.planes, tile_rows(rows)), dev_status), p.cols, le, s);
         if (e == cudaSuccess) e = join_blocks(p, stats, rows, dev_labels + r0, label_logit, dev_loss + r0, dev_lse + r0, nullptr, dev_status, s);
     }
     return e == cudaSuccess ? CHICLE_OK : err.cuda(e);

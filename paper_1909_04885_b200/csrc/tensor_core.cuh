@@ -12,7 +12,7 @@
 // Single precision goes through the same kernel: an fp32 matrix, scaled by a power of two so that its largest element
 // lies in [2^14, 2^15), is held as two fp16 planes. Their sum is off by 2^-22 of an element at most (1e-7 on average, what a sum
 // in fp32 is off by, too), and of elements below 2^-17 of the largest by 2^-39 of that. Three products of planes (1+0, 0+1,
-// 0+0) are summed into one accumulator; the fourth is below 2^-22 of a term. `pairs` is 1 or 3.
+// 0+0) are summed into one accumulator; the fourth is below 2^-22 of a term. `pairs` is 1, 3, or 2: A alone in two planes.
 //
 // The tensor cores cut an accumulator off towards zero at every step of 16, about 2^-25 of it on average (measured: sums of
 // 12 000 steps came out 1.3e-5 too small). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices,
@@ -173,9 +173,9 @@ struct Shape {
     int32_t a_rows;         // rows of A that a copy brings: 128, or fewer where C has no more (K-major A, CG = 1 only)
     int32_t cols;           // columns per tile: BN, or fewer (a multiple of 16, CG = 1 only; every epilogue warp keeps some)
     int32_t k_steps;        // slices of kBK of the summed index (per pair of planes)
-    int32_t pairs;          // 1, or 3 for single precision
+    int32_t pairs;          // products of planes: 1, 3 (single precision) or 2 (A in two planes)
     int32_t parts;          // epilogue warps that share a tile's columns
-    int32_t chunk;          // slices summed in one accumulator
+    int32_t chunk;          // slices whose products of planes come one behind the other; kChunked: summed in one accumulator
     int32_t splits;         // the summed index is cut into so many pieces, each a tile of its own
     int32_t group;          // m tiles walked together before the next column of tiles
     int32_t half;           // operands fp16 (else bf16)
@@ -205,8 +205,8 @@ __device__ __forceinline__ Tile tile_of(const Shape &s, int64_t t)
     return r;
 }
 
-// Planes of the three products, smallest first.
-__device__ __forceinline__ int plane_a(int pairs, int q) { return pairs == 3 && q == 0; }
+// Planes of the products, smallest first.
+__device__ __forceinline__ int plane_a(int pairs, int q) { return pairs > 1 && q == 0; }
 __device__ __forceinline__ int plane_b(int pairs, int q) { return pairs == 3 && q == 1; }
 
 template <int CG, int BN> struct Layout {
@@ -227,8 +227,8 @@ __device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { retur
 // Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end,
 // uint32_t (&acc)[N], uint8_t *patch) const`: called by the epilogue warps, lane by lane with N columns col .. of row
 // row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). All lanes
-// call. Epi::kStep: columns that it takes at a time (0: all of the warp's). kChunked: a tile may be of several chunks, and
-// finish gets all columns of the warp.
+// call. kChunked: every chunk has an accumulator, and finish gets the sums of all columns of the warp; else a tile has one, and
+// finish gets Epi::kStep columns at a time (0: all).
 template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s, const Epi epi)
@@ -335,8 +335,9 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             bool ok = true;
             for (int64_t t = first_tile; ok && t < tiles; t += stride) {
                 const Tile tl = tile_of(s, t);
-                for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
-                    const int slices = (min(c0 + s.chunk, tl.last) - c0) * s.pairs;
+                const int step = kChunked ? s.chunk : tl.last - tl.first;
+                for (int c0 = tl.first; c0 < tl.last; c0 += step, ++n_chunk) {
+                    const int slices = (min(c0 + step, tl.last) - c0) * s.pairs;
                     const uint32_t acc = n_chunk & 1;
                     ok = bar_wait(smem_u32(&s_free[acc]), ((n_chunk >> 1) & 1) ^ 1, &s_stop);
                     if (!ok) break;
@@ -377,6 +378,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             const Tile tl = tile_of(s, t);
             const int row0 = (tl.m * CG + (int)rank) * L::kBM + quarter * 32, col = tl.n * s.cols + part * kN;
             const int end = min(s.n, (tl.n + 1) * s.cols); // the tile's columns end here
+            static_assert(Epi::kStep % 32 == 0, "loads are of 32 columns");
             if constexpr (!kChunked) {
                 constexpr int kStep = Epi::kStep ? Epi::kStep : kN;
                 const uint32_t a = n_chunk & 1;

@@ -11,6 +11,9 @@ STEP = 2.0 ** -23
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
 
+FEW = 32  # rows up to which 16-bit P is held in two planes
+
+
 def softmax_reference(x, w, labels, weights=None, scale=1.0):
     """Everything in 64 bits: loss, lse, dx, dw and, for each, the largest error allowed (element by element)."""
     dt = x.dtype
@@ -44,14 +47,15 @@ def softmax_reference(x, w, labels, weights=None, scale=1.0):
     # and of small ones 2^-40 of the largest) and its rounding; fp16 and its planes: of the lifted value, which may be subnormal
     gs = g.abs()[:, None]
     rel = (2 * (off + off_lse) + 16 * STEP)[:, None]
-    off_p = soft * gs * rel + p.abs() * (4 * STEP if single else HALF[dt])
+    planes = single or n <= FEW  # (two planes: the rounding of what the first one is off by; bf16 2^-16)
+    off_p = soft * gs * rel + p.abs() * (4 * STEP if single else HALF[dt] ** 2 + 4 * STEP if planes else HALF[dt])
     if not single:
         off_p = off_p + soft * gs * 2.0 ** -11 + gs * 2.0 ** -40
     if dt != torch.bfloat16:
         off_p = off_p + float(gs.max()) * 2.0 ** -37
     Wa, Xa = W.abs(), X.abs()
     pa = p.abs() + off_p
-    k = 3 if single else 1
+    k = 3 if single else 2 if planes else 1
     tiny = torch.finfo(dt).smallest_normal * 2 * HALF[dt]
     dx, dw = p @ W, p.T @ X
     off_dx = off_p @ Wa + (k * v + 8) * STEP * (pa @ Wa) + HALF[dt] * dx.abs() * (1 + 2 * HALF[dt]) + tiny
