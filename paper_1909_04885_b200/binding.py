@@ -542,6 +542,23 @@ def _raise(st: int, buf):
         raise ChicleError(st, buf.value.decode())
 
 
+@functools.lru_cache(maxsize=1024)
+def _softmax_bytes(x: tuple, w: tuple, grad: bool) -> int:
+    """``chicle_softmax_workspace`` for two (type, rows, cols, ld, address mod 16): a function of these alone."""
+    need = C.c_size_t()
+    if load().chicle_softmax_workspace(C.byref(Dense(*x[:4], x[4] or 16)), C.byref(Dense(*w[:4], w[4] or 16)), int(grad), C.byref(need)) != OK:
+        raise ChicleError(ERR_INVALID_ARG, "x and w must have one type and the same columns, w at least one row")
+    return need.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _embedding_grad_bytes(n: int, rows: int, cols: int) -> int:
+    need = C.c_size_t()
+    if load().chicle_embedding_grad_workspace(n, rows, cols, C.byref(need)) != OK:
+        raise ChicleError(ERR_INVALID_ARG, "sizes out of range")
+    return need.value
+
+
 def _softmax(x, w, labels, grad: bool, weights=None, scale=1.0, status=None):
     import torch
     lib = load()
@@ -553,22 +570,19 @@ def _softmax(x, w, labels, grad: bool, weights=None, scale=1.0, status=None):
     lp = _vector(labels, n, torch.int32, device, "labels")
     wp = None if weights is None else _vector(weights, n, torch.float32, device, "weights")
     sp = _status_ptr(status, device)
-    need = C.c_size_t()
-    if lib.chicle_softmax_workspace(C.byref(dx), C.byref(dw), int(grad), C.byref(need)) != OK:
-        raise ChicleError(ERR_INVALID_ARG, "x and w must have one type and the same columns, w at least one row")
-    ws = _workspace(need.value, x)
-    loss, lse = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
+    need = _softmax_bytes((dx.type, n, dx.cols, dx.ld, (dx.data or 0) % 16), (dw.type, dw.rows, dw.cols, dw.ld, (dw.data or 0) % 16), grad)
+    ws = _workspace(need, x)
+    loss, lse = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
     buf = _errbuf()
     stream, wsp = _raw_stream(device), None if ws is None else ws.data_ptr()
     if not grad:
         _raise(lib.chicle_softmax_loss(device, stream, C.byref(dx), C.byref(dw), lp, loss.data_ptr(), lse.data_ptr(), wsp,
-                                       need.value, sp, buf, _ERR_LEN), buf)
+                                       need, sp, buf, _ERR_LEN), buf)
         return loss, lse
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    gw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+    gx, gw = x.new_empty(x.shape), w.new_empty(w.shape)
     _raise(lib.chicle_softmax_loss_grad(device, stream, C.byref(dx), C.byref(dw), lp, wp, scale, loss.data_ptr(), lse.data_ptr(),
                                         C.byref(Dense(dx.type, n, dx.cols, dx.cols, gx.data_ptr())),
-                                        C.byref(Dense(dw.type, dw.rows, dw.cols, dw.cols, gw.data_ptr())), wsp, need.value, sp, buf,
+                                        C.byref(Dense(dw.type, dw.rows, dw.cols, dw.cols, gw.data_ptr())), wsp, need, sp, buf,
                                         _ERR_LEN), buf)
     return loss, lse, gx, gw
 
@@ -625,13 +639,11 @@ def embedding_grad(ids, grad, rows: int, scale: float = 1.0, out=None, accumulat
     elif out.get_device() != device or out.shape[0] != rows:
         raise ValueError("out must have `rows` rows and be on the gradient's device")
     dt = _dense(out, "out")
-    need = C.c_size_t()
-    if lib.chicle_embedding_grad_workspace(dg.rows, rows, dg.cols, C.byref(need)) != OK:
-        raise ChicleError(ERR_INVALID_ARG, "sizes out of range")
-    ws = _workspace(need.value, grad)
+    need = _embedding_grad_bytes(dg.rows, rows, dg.cols)
+    ws = _workspace(need, grad)
     buf = _errbuf()
     _raise(lib.chicle_embedding_grad(device, _raw_stream(device), ip, C.byref(dg), scale, int(bool(accumulate)), C.byref(dt),
-                                     None if ws is None else ws.data_ptr(), need.value, _status_ptr(status, device), buf, _ERR_LEN), buf)
+                                     None if ws is None else ws.data_ptr(), need, _status_ptr(status, device), buf, _ERR_LEN), buf)
     return out
 
 

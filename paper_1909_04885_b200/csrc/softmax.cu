@@ -19,6 +19,7 @@
 // rounding of the result: together 1.41 times the result's alone, more where one row decides. (Exponentials in 16 bits with half
 // of fp16's step, no sign bit, changed nothing.)
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "operators.cuh"
@@ -639,7 +640,15 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int 
     s.cols = cols;
     auto *kernel = tc::k_product<CG, BN, AMN, BMN, kChunked, Epi>;
     s.parts = tc::kEpiWarps / 4;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
+    // (once per device and process: 0.5 us a call)
+    static std::atomic<uint64_t> allowed{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (e == cudaSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
+        if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)s.m_tiles * s.n_tiles * s.splits;
     cudaLaunchConfig_t cfg{};
@@ -655,8 +664,8 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int 
     return cudaLaunchKernelEx(&cfg, kernel, ma, mb, s, epi);
 }
 
-// Which tiles. Pairs of CTAs (256 rows) wherever C has more rows than one CTA takes: each fetches half of B (8192 x 131072 x 4096
-// with gradients 23.8 against 23.5 ms, 1777 x 50001 x 1000 823 against 670 us).
+// Which tiles. Pairs of CTAs (256 rows) wherever C has more rows than one CTA takes: each fetches half of B (single CTAs: 23.8 ms for
+// 8192 x 131072 x 4096 with gradients, pairs 23.5; 1777 x 50001 x 1000: 823 and 670 us).
 bool pairs_of_ctas(int64_t m) { return m > 128; }
 // Columns per tile: 128 where C has no more, else 256.
 int tile_columns(int64_t n) { return n <= 128 ? 128 : 256; }
@@ -713,12 +722,12 @@ int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs)
 {
     const int rows = tile_rows(m), cols = tile_columns(n);
     const int64_t tiles = ceil_div(m, rows) * ceil_div(n, cols), slots = kSms / (rows / 128);
-    const double slice = cols == 256 ? 0.28e-6 : 0.15e-6;
+    const double slice = cols == 256 ? 0.28e-6 : 0.25e-6; // (narrow tiles wait for their copies: three quarters of the bytes)
     int best = 1;
     double best_t = 0;
     for (int s = 1; s <= 64 && s <= steps; ++s) {
         const double waves = (double)ceil_div(tiles * s, slots);
-        const double t = waves * ((double)(ceil_div(steps, s) * pairs) * slice + 1.0e-6) + (s > 1 ? 3e-6 + (double)s * m * n * 8.0 / 5e12 : 0.0);
+        const double t = waves * ((double)(ceil_div(steps, s) * pairs) * slice + 1.0e-6) + (s > 1 ? 6e-6 + (double)s * m * n * 8.0 / 5e12 : 0.0);
         if (s == 1 || t < best_t * 0.95) {
             best = s;
             best_t = t;
@@ -765,9 +774,9 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     p.ld_v = (p.v + 63) / 64 * 64;
     // Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential
     // takes on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 512:
-    // 7e-7, 256: 4e-7); all of them where a gradient is rounded to 16 bits in the end.
+    // 7e-7, 256: 4e-7). A gradient that is rounded to 16 bits in the end has one accumulator for all of them.
     p.logit_chunk = (p.wide ? 512 : 1024) / tc::kBK;
-    p.grad_chunk = (p.wide ? 512 : 1024) / tc::kBK; // (16 bits: one accumulator, what is fetched again is in L2 still)
+    p.grad_chunk = (p.wide ? 512 : 1024) / tc::kBK; // (16 bits, P in two planes: what is fetched again is still in L2)
     p.parts = tc::kEpiWarps / 4;
     p.cols = logit_columns(p.n, p.v, p.parts, grad);
     size_t at = 0;

@@ -79,8 +79,8 @@ def check_grad(ops, ids, grad, v, scale, into=None):
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("n,v,d,kind", [
     (1, 1, 1, "flat"), (1, 5, 16, "none"), (7, 3, 5, "mixed"), (8, 4, 8, "one"), (100, 1000, 64, "mixed"), (4096, 300, 40, "mixed"),
-    (4097, 300, 40, "mixed"), (5000, 70000, 33, "flat"), (9000, 17, 1024, "mixed"), (20000, 1, 16, "one"), (30000, 3000000, 8, "mixed"),
-    (140000, 1200, 20, "mixed"), (6000, 900, 2100, "mixed"), (10000, 40, 12, "none"), (300000, 1023, 4, "mixed"), (300000, 1024, 4, "mixed")])
+    (4097, 300, 40, "mixed"), (8192, 5000, 20, "mixed"), (8193, 5000, 20, "mixed"), (5000, 70000, 33, "flat"), (9000, 17, 1024, "mixed"), (20000, 1, 16, "one"), (30000, 3000000, 8, "mixed"),
+    (140000, 1200, 20, "mixed"), (6000, 900, 2100, "mixed"), (9001, 900, 2100, "mixed"), (8500, 17, 1024, "one"), (10000, 40, 12, "none"), (300000, 1023, 4, "mixed"), (300000, 1024, 4, "mixed")])
 def test_gradient(ops, n, v, d, kind, dtype):
     g = torch.Generator(device="cuda").manual_seed(5)
     grad = torch.randn(n, d, generator=g, device="cuda").to(dtype)
@@ -105,7 +105,7 @@ def test_gradient_added_to_what_is_there(ops, n, dtype):
     assert torch.isnan(keep2[v // 2:]).all() and not torch.isnan(keep2[:v // 2]).any()
 
 
-@pytest.mark.parametrize("n", [200, 8000])
+@pytest.mark.parametrize("n", [200, 8000, 9000])
 def test_gradient_of_strided_rows(ops, n):
     wide = torch.randn(n, 90, device="cuda", dtype=torch.bfloat16)
     ids = some_ids(n, 40)
@@ -115,7 +115,7 @@ def test_gradient_of_strided_rows(ops, n):
     assert (out[:, :5] == 3).all() and (out[:, 69:] == 3).all()
 
 
-@pytest.mark.parametrize("n", [50, 6000])
+@pytest.mark.parametrize("n", [50, 6000, 9000])
 def test_ids_beyond_the_last_row(ops, n):
     ids = some_ids(n, 30, kind="flat")
     bad, without = ids.clone(), ids.clone()
@@ -162,6 +162,25 @@ def test_captured(ops, n):
     torch.cuda.synchronize()
     assert torch.equal(out, ops.embedding(table, ids, scale=2.0))
     assert torch.equal(back, ops.embedding_grad(ids, grad, 300, scale=2.0))
+
+
+def test_a_table_beyond_32_bit_offsets(ops):
+    """2.2 G elements: rows in front of and behind element 2^31, and behind byte 2^32."""
+    v, d = 1_100_000, 2048
+    table = torch.empty(v, d, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 1, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 2 ** 21 // 2 + 5000, v - 2, v - 1], device="cuda")
+    table[rows] = torch.randn(8, d, device="cuda").bfloat16()
+    ids = rows.int().repeat(700)
+    assert torch.equal(ops.embedding(table, ids), table[rows].repeat(700, 1))
+    grad = torch.randn(len(ids), d, device="cuda").bfloat16()
+    for n in (64, 5600):  # sorted by counting, and by radix passes
+        table.fill_(1.0)
+        got = ops.embedding_grad(ids[:n], grad[:n], v, out=table)
+        want = grad[:n].double().view(-1, 8, d).sum(0)
+        off = n * STEP * grad[:n].double().abs().view(-1, 8, d).sum(0)
+        assert ((got[rows].double() - want).abs() <= off + HALF[torch.bfloat16] * (want.abs() + off)).all()
+        got[rows] = 0
+        assert not got.any()
 
 
 def test_refusals(ops):

@@ -181,6 +181,34 @@ def test_several_pieces(ops, dtype):
         check(t, want[name], name)
 
 
+def test_weights_beyond_32_bit_offsets(ops):
+    """2.2 G elements of W, labels at both ends: loss, dX, and rows of dW around element 2^31."""
+    n, v, d = 3, 530000, 4096
+    g = torch.Generator(device="cuda").manual_seed(4)
+    w = torch.empty(v, d, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, v, 53000):
+        w[a:a + 53000] = (torch.randn(53000, d, generator=g, device="cuda") / 32).bfloat16()
+    x = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+    labels = torch.tensor([0, 2 ** 19, v - 1], dtype=torch.int32, device="cuda")
+    loss, lse, dx, dw = ops.softmax_loss_grad(x, w, labels)
+    assert all(torch.equal(s, t) for s, t in zip(ops.softmax_loss(x, w, labels), (loss, lse)))
+    X = x.double()
+    logits = torch.cat([X @ w[a:a + 53000].double().T for a in range(0, v, 53000)], 1)
+    total = torch.logsumexp(logits, 1)
+    mine = logits.gather(1, labels.long()[:, None])[:, 0]
+    # logits of 4096 products of magnitude 1/32 on average: the worst case of their sums (operator_util), and the largest logit's rounding
+    off = d * 2.0 ** -23 * float((X.abs() @ w[:53000].double().abs().T).max()) * 1.2 + 2.0 ** -18
+    assert ((lse.double() - total).abs() <= off).all() and ((loss.double() - (total - mine)).abs() <= 2 * off).all()
+    p = (logits - total[:, None]).exp()
+    p[torch.arange(n), labels.long()] -= 1.0
+    want = sum(p[:, a:a + 53000] @ w[a:a + 53000].double() for a in range(0, v, 53000))
+    # the label's row of W decides: P's rounding and the result's, and the logits' error
+    assert ((dx.double() - want).abs() <= (2.0 ** -8 + 4 * off) * (p.abs().max(1, keepdim=True).values * 0.2 + want.abs())).all()
+    for c in (0, 1, 2 ** 19 - 1, 2 ** 19, 2 ** 19 + 1, v - 2, v - 1):
+        ref = p[:, c] @ X
+        assert ((dw[c].double() - ref).abs() <= (2.0 ** -7 + 4 * off) * (p[:, c].abs() @ X.abs())).all()
+
+
 def test_loss_of_many_rows(ops):
     """So many rows that the loss takes them in pieces: rows around the pieces' ends."""
     n, v, d = 180000, 100000, 16
