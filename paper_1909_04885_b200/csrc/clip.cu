@@ -190,7 +190,8 @@ bool results_overlap(const chicle_tensor_t *x, int64_t count)
         if (b) spans.push_back({b, b + bytes, true});
         if (a != b) spans.push_back({a, a + bytes, false});
     }
-    std::sort(spans.begin(), spans.end(), [](const Span &p, const Span &q) { return p.from < q.from; });
+    const auto before = [](const Span &p, const Span &q) { return p.from < q.from; };
+    if (!std::is_sorted(spans.begin(), spans.end(), before)) std::sort(spans.begin(), spans.end(), before);
     uintptr_t any = 0, written = 0; // where the spans so far end
     for (const Span &s : spans) {
         if (s.from < (s.written ? any : written)) return true;

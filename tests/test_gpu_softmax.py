@@ -171,6 +171,32 @@ def test_on_another_stream_and_captured(ops):
         assert all(torch.equal(s, t) for s, t in zip(out, want2))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_many_passes_on_two_streams(ops, dtype):
+    """Captured passes one behind the other on two streams at once: the kernels of one follow those of the other on the same SMs.
+    No wait runs out, and every pass gives the bits of the first."""
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    batches = [inputs(700, 1300, 200, dtype, seed=k, without=0.1) for k in range(2)]
+    first = [ops.softmax_loss_grad(*b[:3], weights=b[3], status=status) for b in batches]
+    torch.cuda.synchronize()
+    graphs, last = [], []
+    for b in batches:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(10):
+                out = ops.softmax_loss_grad(*b[:3], weights=b[3], status=status)
+        graphs.append(graph)
+        last.append(out)
+    streams = [torch.cuda.Stream() for _ in batches]
+    for _ in range(20):
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    assert all(torch.equal(s, t) for a, b in zip(first, last) for s, t in zip(a, b))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=NAMES.get)
 def test_several_pieces(ops, dtype):
     """So many classes that the rows are taken in pieces: dW is summed over them."""
