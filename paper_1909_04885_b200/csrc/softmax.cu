@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ p
     const float f = factor_of(scale, scale_b);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
         Quad v{};
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < splits; ++k) {
             const Quad o = reinterpret_cast<const Quad *>(partial)[(int64_t)k * all + i];
 #pragma unroll
@@ -469,24 +469,29 @@ __device__ __forceinline__ float block_largest(float top)
     return top;
 }
 
-// Largest finite magnitudes, one word per CTA: the first kMaxBlocks of X (rows with a label, where labels are given), the next of W.
+// Largest finite magnitudes, one word per CTA: kMaxBlocks CTAs for X (rows with a label), as many for W and for the weights
+// times the scale, of these groups the ones from `first` on.
 constexpr int kMaxBlocks = 148 * 4;
 
 __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, int64_t ld_x, int64_t n, const int32_t *__restrict__ labels,
                                                  int32_t classes, const float *__restrict__ w, int64_t ld_w, int32_t d,
-                                                 float *__restrict__ largest)
+                                                 const float *__restrict__ weights, float scale, int first_group, float *__restrict__ largest)
 {
-    const bool of_x = blockIdx.x < kMaxBlocks;
-    const float *src = of_x ? x : w;
-    const int64_t ld = of_x ? ld_x : ld_w, rows = of_x ? n : classes;
-    const bool quads = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && (ld & 3) == 0 && (d & 3) == 0;
+    const int group = first_group + (int)blockIdx.x / kMaxBlocks, block = (int)blockIdx.x % kMaxBlocks;
+    const int64_t first = (int64_t)block * 256 + threadIdx.x, step = (int64_t)kMaxBlocks * 256;
     float top = 0.f;
     auto take = [&](float v) {
         v = fabsf(v);
         if (v < INFINITY) top = fmaxf(top, v);
     };
-    const int64_t first = (int64_t)(blockIdx.x % kMaxBlocks) * 256 + threadIdx.x, step = (int64_t)kMaxBlocks * 256;
-    if (!of_x && quads && ld == d) { // no rows to be told apart: 134 MB in 24 us instead of 47
+    const bool of_x = group == 0;
+    const float *src = of_x ? x : w;
+    const int64_t ld = of_x ? ld_x : ld_w, rows = of_x ? n : classes;
+    const bool quads = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && (ld & 3) == 0 && (d & 3) == 0;
+    if (group == 2) {
+#pragma unroll 4
+        for (int64_t i = first; i < n; i += step) take(weights[i] * scale);
+    } else if (!of_x && quads && ld == d) { // no rows to be told apart: 134 MB in 24 us instead of 47
         const float4 *flat = reinterpret_cast<const float4 *>(src);
         const int64_t all = rows * (d / 4);
 #pragma unroll 8
@@ -511,7 +516,7 @@ __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, in
         }
     }
     top = block_largest(top);
-    if (threadIdx.x == 0) largest[blockIdx.x] = top;
+    if (threadIdx.x == 0) largest[group * kMaxBlocks + block] = top;
 }
 
 // One of the matrices that k_pack lays out. `lift`: words of Scales that its scale goes to (single precision).
@@ -525,7 +530,9 @@ struct Packed {
 };
 
 // Rows in a layout that the bulk copies take (whole lines), single precision scaled and as two fp16 planes. The first CTA of
-// a launch also finds the scale of P where there is one.
+// a launch also finds the scale of P where there is one: from the weights themselves while they are few.
+constexpr int64_t kFewWeights = 4096;
+
 template <typename T, typename P>
 __global__ void __launch_bounds__(256) k_pack(const Packed x, const Packed w, int32_t d, int64_t pitch, int32_t classes,
                                               const float *__restrict__ largest, const float *__restrict__ weights, int64_t n, float scale,
@@ -536,8 +543,10 @@ __global__ void __launch_bounds__(256) k_pack(const Packed x, const Packed w, in
     const unsigned block = of_x ? blockIdx.x : blockIdx.x - x.blocks;
     if (scales && blockIdx.x == 0) {
         float top = 0.f;
-        if (weights) {
-#pragma unroll 4
+        if (weights && n > kFewWeights) {
+            for (int i = threadIdx.x; i < kMaxBlocks; i += 256) top = fmaxf(top, largest[2 * kMaxBlocks + i]);
+        } else if (weights) {
+#pragma unroll 16
             for (int64_t i = threadIdx.x; i < n; i += 256) {
                 const float v = fabsf(weights[i] * scale);
                 if (v < INFINITY) top = fmaxf(top, v);
@@ -820,7 +829,7 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
         if (part) p.partial = take(part);
     }
     p.scales = take(kScales * sizeof(float));
-    if (p.wide) p.largest = take(2 * kMaxBlocks * sizeof(float));
+    if (p.half) p.largest = take(3 * kMaxBlocks * sizeof(float));
     p.total = at;
     return p;
 }
@@ -832,9 +841,12 @@ cudaError_t pack(const chicle_dense_t &X, const chicle_dense_t &W, const Plan &p
 {
     *scales = p.wide || (p.half && grad) ? reinterpret_cast<float *>(ws + p.scales) : nullptr;
     float *largest = nullptr;
-    if (p.wide) {
+    const bool many = *scales && weights && p.n > kFewWeights;
+    if (p.wide || many) {
         largest = reinterpret_cast<float *>(ws + p.largest);
-        k_largest<<<2 * kMaxBlocks, 256, 0, s>>>((const float *)X.data, X.ld, p.n, labels, (int32_t)p.v, (const float *)W.data, W.ld, (int32_t)p.d, largest);
+        const int first = p.wide ? 0 : 2, groups = (many ? 3 : 2) - first;
+        k_largest<<<(unsigned)(groups * kMaxBlocks), 256, 0, s>>>((const float *)X.data, X.ld, p.n, labels, (int32_t)p.v, (const float *)W.data, W.ld,
+                                                                  (int32_t)p.d, weights, scale, first, largest);
     }
     auto part = [&](const chicle_dense_t &m, bool is_packed, size_t at, const int32_t *rows_with, int lift) {
         const int64_t blocks = is_packed ? std::min<int64_t>(ceil_div(m.rows * (p.pitch_d / 8), 256), kSms * 16) : 0;
@@ -936,6 +948,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
         q.rows = rows, q.cols = p.v, q.pitch = p.ld_v, q.plane = p.piece * p.ld_v, q.planes = p.p_planes;
         const int steps = p.v >= 8192 ? 4 : 1;
         constexpr int kMany = kWide ? 2 : 1; // planes of P where rows are many
+        const unsigned threads = p.v <= 1024 ? 128 : 256; // (one CTA for the row, then: the other threads would have nothing to do)
         auto *probabilities = p.p_planes != kMany ? (steps == 4 ? k_probabilities<PT, kWide, 2, 4, false>
                                                      : joins    ? k_probabilities<PT, kWide, 2, 1, true>
                                                                 : k_probabilities<PT, kWide, 2, 1, false>)
@@ -943,7 +956,7 @@ cudaError_t run_grad(const Plan &p, const chicle_dense_t &X, const chicle_dense_
                               : joins             ? k_probabilities<PT, kWide, kMany, 1, true>
                                                   : k_probabilities<PT, kWide, kMany, 1, false>;
         for (int64_t y = 0; y < rows; y += 65535)
-            probabilities<<<dim3((unsigned)ceil_div(p.v, 2048 * steps), (unsigned)std::min<int64_t>(65535, rows - y)), 256, 0, stream>>>(store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
+            probabilities<<<dim3((unsigned)ceil_div(p.v, 2048 * steps), (unsigned)std::min<int64_t>(65535, rows - y)), threads, 0, stream>>>(store + y * p.ld_v, prob + y * p.ld_v, p.ld_v, q.plane, (int32_t)rows, (int32_t)p.v, stats + y, norm + y, loss + r0 + y,
                 labels + r0 + y, weights ? weights + r0 + y : nullptr, scale, scales ? scales + kLift : nullptr,
                 __builtin_ctz(tile_columns(p.v) / p.parts), (int)blocks_of(p.v, p.cols, p.parts), label_logit + y, lse + r0 + y, status);
         if ((e = cudaGetLastError()) != cudaSuccess) break;

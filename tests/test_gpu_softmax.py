@@ -46,6 +46,18 @@ def test_gradients(ops, n, v, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("n", [4096, 4097, 9000])
+def test_weights_of_very_different_size(ops, n, dtype):
+    """One weight 2^12 times the others, at the end: P's scale goes by the largest, few weights and many."""
+    x, w, labels, weights = inputs(n, 70, 40, dtype, without=0.1)
+    weights[-1] = 2.0 ** 12
+    labels[-1] = 3
+    want = softmax_reference(x, w, labels, weights, 2.0 ** -20)
+    for name, t in zip(("loss", "lse", "dx", "dw"), ops.softmax_loss_grad(x, w, labels, weights=weights, scale=2.0 ** -20)):
+        check(t, want[name], name)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 def test_equal_inputs_give_equal_bits(ops, dtype):
     x, w, labels, weights = inputs(700, 3000, 200, dtype, without=0.1)
     a = ops.softmax_loss_grad(x, w, labels, weights=weights, scale=0.01)
