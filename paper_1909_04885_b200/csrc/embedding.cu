@@ -558,12 +558,10 @@ cudaError_t sort_ids(const IdPlan &p, const int32_t *ids, int64_t n, int32_t row
     return e;
 }
 
-int size_of(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
-
 // Elements per access: the largest power of two up to 16 bytes that divides addresses, row pitches and the row length.
 int vector_elements(const chicle_dense_t &a, const chicle_dense_t &b)
 {
-    const int es = size_of(a.type);
+    const int es = element_size(a.type);
     uint64_t bits = 16u | reinterpret_cast<uintptr_t>(a.data) | reinterpret_cast<uintptr_t>(b.data) | (uint64_t)a.cols * es;
     if (a.rows > 1) bits |= (uint64_t)a.ld * es;
     if (b.rows > 1) bits |= (uint64_t)b.ld * es;
@@ -619,14 +617,6 @@ template <typename F> cudaError_t by_type(chicle_dtype_t t, int e, F f)
     if (t == CHICLE_F32) return by_width<float>(e, f);
     if (t == CHICLE_BF16) return by_width<__nv_bfloat16>(e, f);
     return by_width<__half>(e, f);
-}
-
-bool overlapping(const chicle_dense_t &a, const chicle_dense_t &b)
-{
-    if (a.rows == 0 || b.rows == 0) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
-    const uintptr_t an = (uintptr_t)((a.rows - 1) * a.ld + a.cols) * size_of(a.type), bn = (uintptr_t)((b.rows - 1) * b.ld + b.cols) * size_of(b.type);
-    return a0 < b0 + bn && b0 < a0 + an;
 }
 
 const char *check_pair(const chicle_dense_t *a, const chicle_dense_t *b, float scale)
@@ -685,7 +675,7 @@ extern "C" chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, 
     const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = cudaSuccess;
     if (n == 0) {
-        const size_t es = (size_t)size_of(dtable->type);
+        const size_t es = (size_t)element_size(dtable->type);
         if (!accumulate && dtable->rows > 0)
             e = cudaMemset2DAsync(dtable->data, (size_t)dtable->ld * es, 0, (size_t)dtable->cols * es, (size_t)dtable->rows, s);
         return e == cudaSuccess ? CHICLE_OK : err.cuda(e);
@@ -694,9 +684,9 @@ extern "C" chicle_status_t chicle_embedding_grad(int device, void *cuda_stream, 
     int which = 0;
     ZeroJob zero{};
     zero.base = static_cast<uint8_t *>(dtable->data);
-    zero.row_bytes = (int32_t)(dtable->cols * size_of(dtable->type));
-    zero.pitch = dtable->ld * size_of(dtable->type);
-    zero.width = vector_elements(*dtable, *dtable) * size_of(dtable->type);
+    zero.row_bytes = (int32_t)(dtable->cols * element_size(dtable->type));
+    zero.pitch = dtable->ld * element_size(dtable->type);
+    zero.width = vector_elements(*dtable, *dtable) * element_size(dtable->type);
     zero.per = (int32_t)std::max<int64_t>(1, kZeroBytes / zero.row_bytes);
     zero.v1 = accumulate ? 0 : dtable->rows;
     e = sort_ids(p, dev_ids, n, (int32_t)dtable->rows, ws, dev_status, s, &which, &zero);

@@ -16,6 +16,18 @@ constexpr int kSms = 148; // B200: grids and workspaces are planned for it, so t
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+inline int element_size(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
+
+// Whether the extents of two matrices have a byte in common.
+inline bool overlapping(const chicle_dense_t &a, const chicle_dense_t &b)
+{
+    if (a.rows == 0 || b.rows == 0) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
+    const uintptr_t an = (uintptr_t)((a.rows - 1) * a.ld + a.cols) * (uintptr_t)element_size(a.type);
+    const uintptr_t bn = (uintptr_t)((b.rows - 1) * b.ld + b.cols) * (uintptr_t)element_size(b.type);
+    return a0 < b0 + bn && b0 < a0 + an;
+}
+
 // nullptr, or what is wrong with the description.
 const char *check_dense(const chicle_dense_t *x);
 

@@ -715,8 +715,6 @@ cudaError_t run_logits(const Operand &a, const Operand &b, const tc::Shape &s, i
     return s.k_steps > s.chunk ? run_product<false, false, true>(a, b, s, cols, epi, stream) : run_product<false, false, false>(a, b, s, cols, epi, stream);
 }
 
-int element_size(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
-
 // Bytes per logit of a piece of rows: 16-bit values in place, or fp32 values and two planes.
 int64_t logit_bytes(bool wide) { return wide ? 8 : 2; }
 
@@ -1002,15 +1000,6 @@ using namespace chicle;
 
 namespace {
 
-bool overlap(const chicle_dense_t &a, const chicle_dense_t &b)
-{
-    if (a.rows == 0 || b.rows == 0) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
-    const uintptr_t an = (uintptr_t)((a.rows - 1) * a.ld + a.cols) * (uintptr_t)element_size(a.type);
-    const uintptr_t bn = (uintptr_t)((b.rows - 1) * b.ld + b.cols) * (uintptr_t)element_size(b.type);
-    return a0 < b0 + bn && b0 < a0 + an;
-}
-
 const char *check_softmax(const chicle_dense_t *X, const chicle_dense_t *W, chicle_status_t *st)
 {
     *st = CHICLE_ERR_INVALID_ARG;
@@ -1081,7 +1070,7 @@ extern "C" chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_strea
     if (const char *m = check_dense(dW)) return err(CHICLE_ERR_INVALID_ARG, m);
     if (dX->type != X->type || dX->rows != X->rows || dX->cols != X->cols) return err(CHICLE_ERR_INVALID_ARG, "dX must have X's type and shape");
     if (dW->type != W->type || dW->rows != W->rows || dW->cols != W->cols) return err(CHICLE_ERR_INVALID_ARG, "dW must have W's type and shape");
-    if (overlap(*dX, *W) || overlap(*dW, *X) || overlap(*dW, *W) || overlap(*dX, *X) || overlap(*dX, *dW))
+    if (overlapping(*dX, *W) || overlapping(*dW, *X) || overlapping(*dW, *W) || overlapping(*dX, *X) || overlapping(*dX, *dW))
         return err(CHICLE_ERR_INVALID_ARG, "dX and dW must not overlap X, W or each other");
     if (!std::isfinite(scale)) return err(CHICLE_ERR_INVALID_ARG, "scale must be finite");
     if (X->rows > 0 && (!dev_labels || !dev_loss || !dev_lse))
