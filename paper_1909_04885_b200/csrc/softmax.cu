@@ -470,7 +470,7 @@ __device__ __forceinline__ float block_largest(float top)
 }
 
 // Largest finite magnitudes, one word per CTA: kMaxBlocks CTAs for X (rows with a label), as many for W and for the weights
-// times the scale, of these groups the ones from `first` on.
+// times the scale (of rows with a label), of these groups the ones from `first` on.
 constexpr int kMaxBlocks = 148 * 4;
 
 __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, int64_t ld_x, int64_t n, const int32_t *__restrict__ labels,
@@ -490,7 +490,8 @@ __global__ void __launch_bounds__(256) k_largest(const float *__restrict__ x, in
     const bool quads = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && (ld & 3) == 0 && (d & 3) == 0;
     if (group == 2) {
 #pragma unroll 4
-        for (int64_t i = first; i < n; i += step) take(weights[i] * scale);
+        for (int64_t i = first; i < n; i += step)
+            if ((uint32_t)labels[i] < (uint32_t)classes) take(weights[i] * scale);
     } else if (!of_x && quads && ld == d) { // no rows to be told apart: 134 MB in 24 us instead of 47
         const float4 *flat = reinterpret_cast<const float4 *>(src);
         const int64_t all = rows * (d / 4);
@@ -530,7 +531,8 @@ struct Packed {
 };
 
 // Rows in a layout that the bulk copies take (whole lines), single precision scaled and as two fp16 planes. The first CTA of
-// a launch also finds the scale of P where there is one: from the weights themselves while they are few.
+// a launch also finds the scale of P where there is one: from the weights themselves (of X's rows with a label) while they are
+// few.
 constexpr int64_t kFewWeights = 4096;
 
 template <typename T, typename P>
@@ -549,7 +551,7 @@ __global__ void __launch_bounds__(256) k_pack(const Packed x, const Packed w, in
 #pragma unroll 16
             for (int64_t i = threadIdx.x; i < n; i += 256) {
                 const float v = fabsf(weights[i] * scale);
-                if (v < INFINITY) top = fmaxf(top, v);
+                if ((uint32_t)x.labels[i] < (uint32_t)classes && v < INFINITY) top = fmaxf(top, v);
             }
         } else {
             top = fabsf(scale);
