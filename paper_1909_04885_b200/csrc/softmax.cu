@@ -59,6 +59,14 @@ __device__ __forceinline__ float exp2_of(float x)
 // inverses. P is scaled wherever it is held in fp16, X and W in single precision.
 enum { kLift, kInvLift, kLiftX, kInvX, kLiftW, kInvW, kScales };
 
+// v times both powers of two, one after the other, the smaller one first: their product may leave fp32's range where the result
+// does not (operands of 1e-20 each, or rows of zeros beside rows of 1e25).
+struct TwoScales {
+    float small, large;
+    __device__ __forceinline__ TwoScales(float a, float b) : small(fminf(a, b)), large(fmaxf(a, b)) {}
+    __device__ __forceinline__ float operator()(float v) const { return (v * small) * large; }
+};
+
 // ---- epilogues ---------------------------------------------------------------------------------------------
 
 // Reduces a tile of logits to (largest, sum of exponentials) per row and N classes, keeps the label's logit, and
@@ -78,7 +86,7 @@ template <typename StoreT> struct LogitsEpilogue {
     {
         const int row = row0 + lane;
         const bool live = row < s.m;
-        const float factor = scales ? scales[kInvX] * scales[kInvW] : 1.f; // of an accumulator, to a logit
+        const TwoScales logit(scales ? scales[kInvX] : 1.f, scales ? scales[kInvW] : 1.f); // of an accumulator
         const int lab = live ? labels[row] - c0 : -1; // (a negative label is in front of every block)
         if (c0 + N > end) {
 #pragma unroll
@@ -99,12 +107,15 @@ template <typename StoreT> struct LogitsEpilogue {
                 for (int w = 8; w > 0; w >>= 1)
 #pragma unroll
                     for (int j = 0; j < w; ++j) q[j] = (lab & w) ? q[w + j] : q[j];
-                label_logit[row] = __uint_as_float(q[0]) * factor;
+                label_logit[row] = logit(__uint_as_float(q[0]));
             }
         // (a block without a logit above -inf: relative to 0, so that its exponentials are 0 and not NaN)
         const float ref = top == -INFINITY ? 0.f : top;
         uint64_t sum[2] = {0, 0}; // pairs of floats
-        const uint64_t back = pair_of(-ref, -ref), to_log2 = pair_of(kLog2e * factor, kLog2e * factor);
+        // (differences are -inf, 0 or of 2^-48 to 2^48: kept within fp32's range, the factor leaves of them what the true one
+        // does, and 0 and -inf as they are)
+        const float factor = fminf(fmaxf(logit(kLog2e), 0x1p-126f), 0x1p126f);
+        const uint64_t back = pair_of(-ref, -ref), to_log2 = pair_of(factor, factor);
         constexpr int kWidth = sizeof(StoreT) >= 2 ? 64 / (int)sizeof(StoreT) : N; // columns of a patch
         constexpr int kPer = sizeof(StoreT) >= 2 ? 16 / (int)sizeof(StoreT) : 8;    // and of a piece
 #pragma unroll
@@ -143,7 +154,7 @@ template <typename StoreT> struct LogitsEpilogue {
             }
         }
         // NaN: fmaxf passes over it, the sum does not
-        if (live && c0 < end) stats[(int64_t)(tl.n * s.parts + (c0 - tl.n * s.cols) / N) * s.m + row] = make_float2(top * factor, (low_of(sum[0]) + low_of(sum[1])) + (high_of(sum[0]) + high_of(sum[1])));
+        if (live && c0 < end) stats[(int64_t)(tl.n * s.parts + (c0 - tl.n * s.cols) / N) * s.m + row] = make_float2(logit(top), (low_of(sum[0]) + low_of(sum[1])) + (high_of(sum[0]) + high_of(sum[1])));
     }
 };
 
@@ -151,7 +162,7 @@ struct NoStore {
     char c;
 };
 
-__device__ __forceinline__ float factor_of(const float *a, const float *b) { return (a ? *a : 1.f) * (b ? *b : 1.f); }
+__device__ __forceinline__ TwoScales scales_of(const float *a, const float *b) { return TwoScales(a ? *a : 1.f, b ? *b : 1.f); }
 
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
@@ -176,7 +187,7 @@ template <typename OutT> struct GradEpilogue {
                                            uint8_t *patch) const
     {
         const bool whole = partial || keep;
-        const float f = whole ? 1.f : factor_of(scale, scale_b);
+        const TwoScales f = whole ? TwoScales(1.f, 1.f) : scales_of(scale, scale_b);
         const uint32_t zeros = __ballot_sync(0xffffffffu, labels && row0 + lane < s.m && (uint32_t)labels[row0 + lane] >= (uint32_t)classes);
         float *dst32 = partial ? partial + (int64_t)tl.split * s.m * s.n : keep;
         const float *src = partial ? nullptr : add;
@@ -189,7 +200,7 @@ template <typename OutT> struct GradEpilogue {
                 for (int c = 0; c < 4; ++c) {
                     alignas(16) OutT q[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j] = from_float<OutT>(zero ? 0.f : __uint_as_float(r[8 * c + j]) * f);
+                    for (int j = 0; j < 8; ++j) q[j] = from_float<OutT>(zero ? 0.f : f(__uint_as_float(r[8 * c + j])));
                     *tc::patch_at(patch, lane, c) = *reinterpret_cast<const uint4 *>(q);
                 }
                 __syncwarp();
@@ -239,7 +250,7 @@ template <typename OutT> struct GradEpilogue {
                     } else {
                         struct alignas(4 * sizeof(OutT)) {
                             OutT v[4];
-                        } q{{from_float<OutT>(v.x * f), from_float<OutT>(v.y * f), from_float<OutT>(v.z * f), from_float<OutT>(v.w * f)}};
+                        } q{{from_float<OutT>(f(v.x)), from_float<OutT>(f(v.y)), from_float<OutT>(f(v.z)), from_float<OutT>(f(v.w))}};
                         *reinterpret_cast<decltype(q) *>(out + (int64_t)row * ld + col) = q;
                     }
                 } else {
@@ -249,7 +260,7 @@ template <typename OutT> struct GradEpilogue {
                         if (col + j < s.n) {
                             const float x = w[j] + (src ? src[at + j] : 0.f);
                             if (whole) dst32[at + j] = x;
-                            else out[(int64_t)row * ld + col + j] = from_float<OutT>(x * f);
+                            else out[(int64_t)row * ld + col + j] = from_float<OutT>(f(x));
                         }
                 }
             }
@@ -267,7 +278,7 @@ __global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ p
         float v[V];
     };
     const int64_t all = m * n / V;
-    const float f = factor_of(scale, scale_b);
+    const TwoScales f = scales_of(scale, scale_b);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
         Quad v{};
 #pragma unroll 8
@@ -288,7 +299,7 @@ __global__ void __launch_bounds__(256) k_join_splits(const float *__restrict__ p
         } else {
             OutT *dst = out + row * ld + (i * V - row * n);
 #pragma unroll
-            for (int j = 0; j < V; ++j) dst[j] = from_float<OutT>(v.v[j] * f);
+            for (int j = 0; j < V; ++j) dst[j] = from_float<OutT>(f(v.v[j]));
         }
     }
 }

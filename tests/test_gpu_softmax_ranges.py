@@ -33,3 +33,36 @@ def test_weights_of_rows_without_a_label(ops, n, dtype):
     for name, t in zip(("loss", "lse", "dx", "dw"), got):
         check(t, want[name], name)
     assert all(torch.equal(s, t) for s, t in zip(got, ops.softmax_loss_grad(x, w, labels, weights=weights, scale=2.0 ** -10)))
+
+
+@pytest.mark.parametrize("size_x,size_w", [(1e-18, 1e-18), (1e-25, 1e-25), (1e-30, 1e30), (1e30, 1e-30), (1e-35, 1e-35)])
+@pytest.mark.parametrize("n,v", [(40, 257), (300, 257), (300, 100), (20, 3), (300, 512)])
+def test_single_precision_of_far_sizes(ops, n, v, size_x, size_w):
+    """Operands far below (and above) one, blocks of classes that are not full: the scales' product leaves fp32's range, the
+    results do not."""
+    x, w, labels, weights = inputs(n, v, 72, torch.float32, without=0.1)
+    x, w = x * size_x, w * size_w
+    want = softmax_reference(x, w, labels, weights, 1.0)
+    loss, lse = ops.softmax_loss(x, w, labels)
+    check(loss, want["loss"], "loss")
+    check(lse, want["lse"], "lse")
+    for name, t in zip(("loss", "lse", "dx", "dw"), ops.softmax_loss_grad(x, w, labels, weights=weights)):
+        check(t, want[name], name)
+
+
+@pytest.mark.parametrize("n,v", [(40, 257), (300, 300)])
+def test_single_precision_of_large_operands_with_logits_of_zero(ops, n, v):
+    """x and w of 1e25 without a column in common: all logits are 0, the loss log(v) (rounded: 2^-20), and the gradients a mean of
+    rows, off by their planes and the sums of 3 v and 3 n products."""
+    x, w, labels, _ = inputs(n, v, 80, torch.float32)
+    x, w = x * 1e25, w * 1e25
+    x[:, 40:], w[:, :40] = 0.0, 0.0
+    loss, lse, dx, dw = ops.softmax_loss_grad(x, w, labels, scale=1.0 / n)
+    for t in (loss, lse) + ops.softmax_loss(x, w, labels):
+        assert ((t.double() - torch.tensor(float(v), dtype=torch.float64).log().item()).abs() <= 2.0 ** -20).all()
+    p = torch.full((n, v), 1.0 / v, dtype=torch.float64, device="cuda")
+    p[torch.arange(n), labels.long()] -= 1.0
+    p /= n
+    for got, a, b, k in ((dx, p, w.double(), v), (dw, p.T, x.double(), n)):
+        off = (3 * k + 32) * 2.0 ** -23 * (a.abs() @ b.abs()) + 2.0 ** -38 * a.abs().sum(1, keepdim=True) * b.abs().max()
+        assert ((got.double() - a @ b).abs() <= off).all()
