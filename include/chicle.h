@@ -362,8 +362,8 @@ typedef struct {
 } chicle_tensor_t;
 
 /* *dev_norm = the 2-norm of all elements of all tensors (squares summed in fp64 in a fixed order), and
- * out = in * min(1, max_norm / (norm + 1e-6)) for each of them. A norm that is not finite leaves the elements as they are
- * (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors is a host array, read
+ * out = in * min(1, max_norm / (norm + 1e-6)) for each of them. A *dev_norm that is not finite (beyond fp32, too) leaves the
+ * elements as they are (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors is a host array, read
  * during the call. An out is the tensor's own in or overlaps neither any in nor another out (a tensor listed twice with a result
  * is refused; without results it counts twice). Workspace: CHICLE_CLIP_WORKSPACE bytes, 256-byte aligned. */
 #define CHICLE_CLIP_WORKSPACE 16384

@@ -157,9 +157,11 @@ __global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table<M> 
     double s = 0.0;
     for (int i = threadIdx.x; i < n_sums; i += 256) s += sums[i];
     const double total = sqrt(block_sum(s));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+    // (what the caller sees decides: a norm beyond fp32 is shown as infinity, and the elements stay)
+    const float shown = (float)total;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = shown;
     const double f64 = (double)max_norm / (total + 1e-6);
-    const float f = f64 < 1.0 && total <= 1.7e308 ? (float)f64 : 1.f; // (a NaN fails both)
+    const float f = f64 < 1.0 && shown < INFINITY ? (float)f64 : 1.f; // (a NaN fails both)
     for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
         const uint32_t c = chunks - 1 - i;
         int64_t at;
