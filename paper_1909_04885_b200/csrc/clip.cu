@@ -127,7 +127,14 @@ __global__ void __launch_bounds__(256) k_squares(const __grid_constant__ Table<M
     if (threadIdx.x == 0) sums[blockIdx.x] = first ? s : sums[blockIdx.x] + s;
 }
 
-template <typename T> __device__ __forceinline__ void chunk_scale(const T *p, T *o, int len, float f)
+// The factor as two: below fp32's normal range it would lose its bits, a power of two in front of it takes them back.
+struct Factor {
+    float power, rest;
+    __device__ __forceinline__ explicit Factor(double f) : power(f < 0x1p-100 ? 0x1p-64f : 1.f), rest((float)(f < 0x1p-100 ? f * 0x1p64 : f)) {}
+    __device__ __forceinline__ float operator()(float v) const { return (v * power) * rest; }
+};
+
+template <typename T> __device__ __forceinline__ void chunk_scale(const T *p, T *o, int len, const Factor &f)
 {
     constexpr int kPer = 16 / (int)sizeof(T);
     // (in and out at different places within 16 bytes: element by element)
@@ -140,13 +147,13 @@ template <typename T> __device__ __forceinline__ void chunk_scale(const T *p, T 
         uint4 x = q[j];
         T *e = reinterpret_cast<T *>(&x);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) e[i] = rounded<T>((float)e[i] * f);
+        for (int i = 0; i < kPer; ++i) e[i] = rounded<T>(f((float)e[i]));
         r[j] = x;
     }
     const int rest = len - vecs * kPer;
     for (int j = threadIdx.x; j < rest; j += 256) {
         const int i = j < head ? j : j + vecs * kPer;
-        o[i] = rounded<T>((float)p[i] * f);
+        o[i] = rounded<T>(f((float)p[i]));
     }
 }
 
@@ -161,12 +168,12 @@ __global__ void __launch_bounds__(256) k_scale(const __grid_constant__ Table<M> 
     const float shown = (float)total;
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = shown;
     const double f64 = (double)max_norm / (total + 1e-6);
-    const float f = f64 < 1.0 && shown < INFINITY ? (float)f64 : 1.f; // (a NaN fails both)
+    const Factor f(f64 < 1.0 && shown < INFINITY ? f64 : 1.0); // (a NaN fails both)
     for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
         const uint32_t c = chunks - 1 - i;
         int64_t at;
         const int k = tensor_of(t, c, at);
-        if (!t.out[k] || (f == 1.f && t.out[k] == t.in[k])) continue;
+        if (!t.out[k] || (f.power * f.rest == 1.f && t.out[k] == t.in[k])) continue;
         const int len = (int)min((int64_t)kChunk, t.n[k] - at);
         if (t.type[k] == CHICLE_F32) chunk_scale(static_cast<const float *>(t.in[k]) + at, static_cast<float *>(t.out[k]) + at, len, f);
         else if (t.type[k] == CHICLE_BF16)

@@ -31,3 +31,19 @@ def test_the_largest_norm_that_fp32_holds(ops):
     t = torch.full((4,), 2.0 ** 126, device="cuda")
     assert float(ops.clip_gradients([t], 2.0 ** 100)) == 2.0 ** 127
     assert torch.equal(t, torch.full((4,), 2.0 ** 99, device="cuda"))
+
+
+@pytest.mark.parametrize("max_norm", [1.0, 1e-3, 1e-6])
+@pytest.mark.parametrize("size", [1e30, 1e34, 3e36])
+def test_factors_below_the_normal_range_of_fp32(ops, size, max_norm):
+    """The norm's error (2^-21), the factor's and the product's roundings (2^-24 each), and results of the type's smallest steps."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    t = [torch.randn(1000, generator=g, device="cuda") * size, (torch.randn(900, generator=g, device="cuda") * size).bfloat16()]
+    before = [x.double() for x in t]
+    norm = math.sqrt(sum(float((b * b).sum()) for b in before))
+    assert norm < 3e38
+    got = ops.clip_gradients(t, max_norm)
+    assert abs(float(got) - norm) <= 2.0 ** -21 * norm
+    for b, x, half in zip(before, t, (2.0 ** -24, 2.0 ** -8)):
+        want = b * (max_norm / (norm + 1e-6))
+        assert ((x.double() - want).abs() <= want.abs() * (2.0 ** -21 + 3 * 2.0 ** -24 + half * (1 + 2.0 ** -20)) + 2.0 ** -126 * 2 * half).all()
