@@ -331,8 +331,9 @@ chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_
 /* The same, and the gradients of  scale * sum_i weight_i loss_i  (dev_weights: one float per row, or NULL for 1; scale
  * finite) with respect to X and W, in their types: every element of dX and dW is written (rows of dX without a label are
  * 0; their weights have no effect either). The rows' weighted differences of probability and label are held to 2^-39 of the
- * largest weight of a row with a label in fp16 and fp32: rows whose weights are further below it lose bits of their gradients. dX and dW overlap neither X, W nor each other. The logits are held for about two gigabytes of rows at a time (8 GB at
- * most), and where there are several such pieces, dW is summed in fp32 in the workspace. */
+ * largest weight of a row with a label in fp16 and fp32: rows whose weights are further below it lose bits of their gradients. dX and dW overlap neither X, W nor each other. The logits are held for about two gigabytes of rows at a time (8 GiB at
+ * most, if that holds a row; beside them a 32nd of that for sums), and where there are several such pieces, dW is summed in fp32
+ * in the workspace. */
 chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
                                          const int32_t *dev_labels, const float *dev_weights, float scale, float *dev_loss,
                                          float *dev_lse, const chicle_dense_t *dX, const chicle_dense_t *dW, void *dev_workspace,

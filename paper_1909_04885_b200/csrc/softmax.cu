@@ -728,8 +728,8 @@ cudaError_t run_logits(const Operand &a, const Operand &b, const tc::Shape &s, i
     return s.k_steps > s.chunk ? run_product<false, false, true>(a, b, s, cols, epi, stream) : run_product<false, false, false>(a, b, s, cols, epi, stream);
 }
 
-// Bytes per logit of a piece of rows: 16-bit values in place, or fp32 values and two planes.
-int64_t logit_bytes(bool wide) { return wide ? 8 : 2; }
+// Bytes per logit of a piece of rows: 16-bit values in place, or 16-bit or fp32 values and two planes.
+int64_t logit_bytes(bool wide, int p_planes) { return wide ? 8 : p_planes == 2 ? 6 : 2; }
 
 bool takes_bulk(const chicle_dense_t &x)
 {
@@ -807,11 +807,15 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     };
     p.piece = p.n;
     if (grad) {
-        int64_t rows = kPieceBytes / (p.ld_v * logit_bytes(p.wide)) / 256 * 256;
+        const int64_t row_bytes = p.ld_v * logit_bytes(p.wide, p.p_planes);
+        const int64_t most = std::max<int64_t>(1, 4 * kPieceBytes / row_bytes);
         // fewer than 2048 rows: the fp32 sums of dW would be read and written too often beside the products of a piece
-        rows = std::max(rows, std::min<int64_t>(2048, 4 * kPieceBytes / (p.ld_v * logit_bytes(p.wide))));
-        rows = std::max<int64_t>(rows, 256);
-        if (rows < p.n) p.piece = ceil_div(ceil_div(p.n, ceil_div(p.n, rows)), 256) * 256;
+        const int64_t rows = std::max(kPieceBytes / row_bytes / 256 * 256, std::min<int64_t>(2048, most));
+        if (rows < p.n) {
+            p.piece = ceil_div(p.n, ceil_div(p.n, rows));
+            const int64_t whole = ceil_div(p.piece, 256) * 256; // (whole tiles, where there is room for them)
+            if (whole <= most) p.piece = whole;
+        }
     } else {
         const int64_t rows = std::max<int64_t>(4096, kStatBytes / (blocks_of(p.v, p.cols, p.parts) * (int64_t)sizeof(float2)) / 256 * 256);
         p.piece = std::min(p.n, rows);
