@@ -508,17 +508,23 @@ def _status_ptr(status, device: int):
 def _operator(fn):
     """Adds the keyword ``stream`` to an operator: the caller's stream is torch's current one while outputs and workspaces
     are allocated and the work is enqueued."""
+    name = fn.__code__.co_varnames[0]  # the first argument, which may be given by its name
+
     @functools.wraps(fn)
     def call(*args, stream: Optional[int] = None, **kw):
-        if stream is None:
+        if stream is None or (not args and name not in kw):
             return fn(*args, **kw)
         import torch
-        first = args[0]
+        first = args[0] if args else kw[name]
         if not isinstance(first, torch.Tensor):  # several: an iterator is used up here
-            args = (list(first),) + args[1:]
-            if not args[0]:
+            several = list(first)
+            if args:
+                args = (several,) + args[1:]
+            else:
+                kw[name] = several
+            if not several:
                 return fn(*args, **kw)
-            first = args[0][0]
+            first = several[0]
         with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=first.device)):
             return fn(*args, **kw)
     return call
