@@ -309,7 +309,8 @@ typedef enum { CHICLE_F32 = 0, CHICLE_BF16 = 1, CHICLE_F16 = 2 } chicle_dtype_t;
 
 /* A caller-owned dense matrix on the device, row-major: element (i, j) at data[i * ld + j], ld >= cols in elements. Any
  * alignment of the element type and any ld are taken; 16-byte aligned rows save a copy. rows may be 0, rows <=
- * 2^31 - 4097, 1 <= cols <= 65536. */
+ * 2^31 - 4097, 1 <= cols <= 65536. Two matrices overlap if they share a byte (matrices of one pitch may lie side by side in
+ * a buffer), or, with different pitches, if their extents from the first element to the last do. */
 typedef struct {
     chicle_dtype_t type;
     int64_t rows, cols, ld;

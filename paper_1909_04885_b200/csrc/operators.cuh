@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cstdio>
 
 #include "chicle_internal.cuh"
@@ -18,14 +19,22 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline int element_size(chicle_dtype_t t) { return t == CHICLE_F32 ? 4 : 2; }
 
-// Whether the extents of two matrices have a byte in common.
+// Whether two matrices have a byte in common. Exact where their rows are equally far apart (or one has a single row), so that
+// they may lie side by side in one buffer; of rows at different distances the extents are compared.
 inline bool overlapping(const chicle_dense_t &a, const chicle_dense_t &b)
 {
     if (a.rows == 0 || b.rows == 0) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
-    const uintptr_t an = (uintptr_t)((a.rows - 1) * a.ld + a.cols) * (uintptr_t)element_size(a.type);
-    const uintptr_t bn = (uintptr_t)((b.rows - 1) * b.ld + b.cols) * (uintptr_t)element_size(b.type);
-    return a0 < b0 + bn && b0 < a0 + an;
+    using Wide = __int128; // (rows times pitch may leave 64 bits)
+    const Wide a0 = reinterpret_cast<uintptr_t>(a.data), b0 = reinterpret_cast<uintptr_t>(b.data);
+    const Wide wa = a.cols * element_size(a.type), wb = b.cols * element_size(b.type); // bytes of a row
+    const Wide pa = (Wide)a.ld * element_size(a.type), pb = (Wide)b.ld * element_size(b.type);
+    if (a0 >= b0 + (b.rows - 1) * pb + wb || b0 >= a0 + (a.rows - 1) * pa + wa) return false;
+    if ((a.rows == 1 && b.rows == 1) || (a.rows > 1 && b.rows > 1 && pa != pb)) return true;
+    // b's row j and a's row i meet where -wb < b0 - a0 + k pitch < wa with k = j - i: the smallest k to the right of -wb decides
+    const Wide pitch = a.rows > 1 ? pa : pb, from = a0 - b0 - wb;
+    const Wide below = from >= 0 ? from / pitch : -((-from + pitch - 1) / pitch); // rounded down
+    const Wide k = std::max<Wide>(below + 1, 1 - a.rows);
+    return k < b.rows && b0 - a0 + k * pitch < wa;
 }
 
 // nullptr, or what is wrong with the description.
