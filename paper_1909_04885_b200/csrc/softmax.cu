@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 
 #include "operators.cuh"
 #include "tensor_core.cuh"
@@ -650,6 +651,17 @@ bool make_map(CUtensorMap *map, const Operand &o, bool half, int box_cols, int b
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Test aid (read once per process): from this tile on the operands of the products are not fetched, and waits are short. -1: none.
+int64_t dropped_copies()
+{
+    static const int64_t drop = [] {
+        const char *env = getenv("CHICLE_TEST_DROP_COPIES");
+        return env ? std::max<int64_t>(0, atoll(env)) : -1;
+    }();
+    return drop;
+}
+constexpr int64_t kTestClocks = 20000000; // 10 to 20 ms
+
 template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
 cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int cols, const Epi &epi, cudaStream_t stream)
 {
@@ -673,6 +685,9 @@ cudaError_t launch_product(const Operand &a, const Operand &b, tc::Shape s, int 
     }
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)s.m_tiles * s.n_tiles * s.splits;
+    const int64_t drop = dropped_copies();
+    s.fetched = drop < 0 ? tiles : std::min(tiles, drop);
+    s.limit = drop < 0 ? tc::kWaitClocks : kTestClocks;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(CG * (tiles < kSms / CG ? tiles : kSms / CG)));
     cfg.blockDim = dim3(tc::kThreads);

@@ -20,7 +20,7 @@
 // chunk the small products of planes come first.
 //
 // Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's copies and products in flight are
-// waited for and tensor memory is given back before it returns.
+// waited for (within the same limit, all of them together) and tensor memory is given back before it returns.
 #pragma once
 
 #include <cuda.h>
@@ -38,7 +38,7 @@ constexpr int kBK = 64;              // summed elements per stage: 128 bytes, on
 constexpr int kEpiWarps = 8;                 // (sixteen with half the columns each: products of 4096 terms 6 % slower, of 64 the same)
 constexpr int kThreads = 64 + 32 * kEpiWarps; // and a copy warp, a product warp
 constexpr uint32_t kPatchBytes = 2048;  // shared memory of an epilogue warp: 32 rows of 64 bytes
-constexpr long long kWaitClocks = 6000000000ll; // some seconds
+constexpr long long kWaitClocks = 6000000000ll; // some seconds: Shape::limit, but for tests
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -63,7 +63,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 // False once the wait has run out, here or in another role of the CTA.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped, long long limit)
 {
     if (bar_try(bar, parity)) return true;
     const long long t0 = clock64();
@@ -72,7 +72,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         for (int i = 0; i < 16; ++i)
             if (bar_try(bar, parity)) return true;
         if (*stopped) return false;
-        if (clock64() - t0 > kWaitClocks) {
+        if (clock64() - t0 > limit) {
             *stopped = 1;
             return false;
         }
@@ -81,18 +81,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 // The epilogue's warps wait for an accumulator: one of their threads looks, the others sleep at a barrier (threads that all
 // look take power and issue slots from the products: dX of 2048 rows, 32768 classes and 4096 columns took 410 us, 396 so). All of
 // them get the same answer.
-__device__ __forceinline__ bool epilogue_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped, volatile uint32_t *answer, bool looks)
+__device__ __forceinline__ bool epilogue_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stopped, long long limit, volatile uint32_t *answer,
+                                              bool looks)
 {
-    if (looks) *answer = bar_wait(bar, parity, stopped);
+    if (looks) *answer = bar_wait(bar, parity, stopped, limit);
     __syncwarp();
     asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
     return *answer != 0;
 }
-// For what is in flight when a CTA stops.
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
+// For what is in flight when a CTA stops. t0: when its drains began; they share one limit.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity, long long t0, long long limit)
 {
-    const long long t0 = clock64();
-    while (!bar_try(bar, parity) && clock64() - t0 <= kWaitClocks) {}
+    while (!bar_try(bar, parity) && clock64() - t0 <= limit) {}
 }
 // The same address in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank)
@@ -141,12 +141,12 @@ __device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint
         asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// The barrier (of both CTAs of a pair) is arrived at when all products issued before are done.
-template <int CG> __device__ __forceinline__ void commit(uint32_t bar)
+// The barrier (of both CTAs of a pair, or of those in `ctas`) is arrived at when all products issued before are done.
+template <int CG> __device__ __forceinline__ void commit(uint32_t bar, uint32_t ctas = 3)
 {
     if constexpr (CG == 2)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+                     ::"r"(bar), "h"((uint16_t)ctas) : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -179,6 +179,8 @@ struct Shape {
     int32_t splits;         // the summed index is cut into so many pieces, each a tile of its own
     int32_t group;          // m tiles walked together before the next column of tiles
     int32_t half;           // operands fp16 (else bf16)
+    int64_t fetched;        // tiles whose operands are fetched: all of them, but for a test of what happens where a copy never comes
+    int64_t limit;          // of a wait, in clocks
     uint32_t *status;       // may be null
 };
 
@@ -283,7 +285,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             bool ok = true;
             // a copy of either CTA of a pair completes at the leader's barrier
             const uint32_t bytes = CG * (uint32_t)(s.a_rows + s.cols / CG) * (kBK * 2);
-            for (int64_t t = first_tile; ok && t < tiles; t += stride) {
+            for (int64_t t = first_tile; ok && t < s.fetched; t += stride) {
                 const Tile tl = tile_of(s, t);
                 const int row = (tl.m * CG + (int)rank) * L::kBM, col = tl.n * s.cols + (int)rank * L::kBNc;
                 for (int c0 = tl.first; ok && c0 < tl.last; c0 += s.chunk) {
@@ -292,7 +294,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                         const int za = plane_a(s.pairs, q), zb = plane_b(s.pairs, q);
                         for (int k = c0; k < c1; ++k, ++it) {
                             const uint32_t st = it % L::kStages, ph = (it / L::kStages) & 1;
-                            if (!bar_wait(smem_u32(&s_empty[st]), ph ^ 1, &s_stop)) {
+                            if (!bar_wait(smem_u32(&s_empty[st]), ph ^ 1, &s_stop, s.limit)) {
                                 ok = false;
                                 break;
                             }
@@ -321,9 +323,10 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             // CTA on the SM then, and an arrival that comes late would count at that one's barrier. So the last use of every
             // stage is waited for. (Stopped: the copies in flight, which complete at the leader's barriers.)
             const uint32_t used = it < (uint32_t)L::kStages ? it : L::kStages;
+            const long long t0 = clock64();
             for (uint32_t j = it - used; j < it; ++j) {
-                if (ok) ok = bar_wait(smem_u32(&s_empty[j % L::kStages]), (j / L::kStages) & 1, &s_stop);
-                else if (rank == 0) bar_drain(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1);
+                if (ok) ok = bar_wait(smem_u32(&s_empty[j % L::kStages]), (j / L::kStages) & 1, &s_stop, s.limit);
+                if (!ok && rank == 0) bar_drain(smem_u32(&s_full[j % L::kStages]), (j / L::kStages) & 1, t0, s.limit);
             }
         }
     } else if (warp == 1) {
@@ -339,13 +342,13 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 for (int c0 = tl.first; c0 < tl.last; c0 += step, ++n_chunk) {
                     const int slices = (min(c0 + step, tl.last) - c0) * s.pairs;
                     const uint32_t acc = n_chunk & 1;
-                    ok = bar_wait(smem_u32(&s_free[acc]), ((n_chunk >> 1) & 1) ^ 1, &s_stop);
+                    ok = bar_wait(smem_u32(&s_free[acc]), ((n_chunk >> 1) & 1) ^ 1, &s_stop, s.limit);
                     if (!ok) break;
                     fence_after();
                     const uint32_t d = tmem + acc * BN;
                     for (int i = 0; i < slices; ++i, ++it) {
                         const uint32_t st = it % L::kStages;
-                        ok = bar_wait(smem_u32(&s_full[st]), (it / L::kStages) & 1, &s_stop);
+                        ok = bar_wait(smem_u32(&s_full[st]), (it / L::kStages) & 1, &s_stop, s.limit);
                         if (!ok) break;
                         fence_after();
                         const uint32_t a = ring + st * L::kStageBytes;
@@ -360,10 +363,10 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 }
             }
             // (and the epilogues' last arrivals, the other CTA's among them)
-            for (uint32_t j = n_chunk < 2 ? 0 : n_chunk - 2; ok && j < n_chunk; ++j) ok = bar_wait(smem_u32(&s_free[j & 1]), (j >> 1) & 1, &s_stop);
+            for (uint32_t j = n_chunk < 2 ? 0 : n_chunk - 2; ok && j < n_chunk; ++j) ok = bar_wait(smem_u32(&s_free[j & 1]), (j >> 1) & 1, &s_stop, s.limit);
             if (s_stop) { // products in flight are waited for before tensor memory is given back
-                commit<CG>(smem_u32(&s_drain));
-                bar_drain(smem_u32(&s_drain), 0);
+                commit<CG>(smem_u32(&s_drain), 1); // (this CTA's barrier alone: the other one waits for nothing there)
+                bar_drain(smem_u32(&s_drain), 0, clock64(), s.limit);
             }
         }
     } else {
@@ -382,7 +385,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             if constexpr (!kChunked) {
                 constexpr int kStep = Epi::kStep ? Epi::kStep : kN;
                 const uint32_t a = n_chunk & 1;
-                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, &s_answer[a], threadIdx.x == 64);
+                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, s.limit, &s_answer[a], threadIdx.x == 64);
                 if (!ok) break;
                 ++n_chunk;
                 fence_after();
@@ -402,7 +405,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             uint32_t acc[kN];
             for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
                 const uint32_t a = n_chunk & 1;
-                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, &s_answer[a], threadIdx.x == 64);
+                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, s.limit, &s_answer[a], threadIdx.x == 64);
                 if (!ok) break;
                 fence_after();
                 if (c0 == tl.first) {
