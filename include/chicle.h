@@ -301,7 +301,7 @@ chicle_status_t chicle_partition_noalloc(int device, void *cuda_stream, int64_t 
  * equal bits. host_errbuf (may be NULL) receives the text of an error; on CHICLE_ERR_INVALID_ARG nothing is enqueued.
  * dev_status (may be NULL) is one word that kernels OR bits into and never clear: CHICLE_STATUS_BAD_ID (a label or id
  * beyond the last class or row: treated as none) and CHICLE_STATUS_TIMEOUT (a bounded wait ran out: the results are
- * not valid). ---- */
+ * not valid, and the losses and gradients that the unfinished work concerns are NaN, whether a status word is given or not). ---- */
 typedef enum { CHICLE_F32 = 0, CHICLE_BF16 = 1, CHICLE_F16 = 2 } chicle_dtype_t;
 
 #define CHICLE_STATUS_BAD_ID 4u

@@ -82,8 +82,8 @@ template <typename StoreT> struct LogitsEpilogue {
     const float *scales;   // single precision: the operands' scales (Scales); else null
 
     template <int N>
-    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, uint32_t (&r)[N],
-                                           uint8_t *patch) const
+    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, bool ok,
+                                           uint32_t (&r)[N], uint8_t *patch) const
     {
         const int row = row0 + lane;
         const bool live = row < s.m;
@@ -111,7 +111,7 @@ template <typename StoreT> struct LogitsEpilogue {
                 label_logit[row] = logit(__uint_as_float(q[0]));
             }
         // (a block without a logit above -inf: relative to 0, so that its exponentials are 0 and not NaN)
-        const float ref = top == -INFINITY ? 0.f : top;
+        const float ref = !ok ? NAN : top == -INFINITY ? 0.f : top;
         uint64_t sum[2] = {0, 0}; // pairs of floats
         // (differences are -inf, 0 or of 2^-48 to 2^48: kept within fp32's range, the factor leaves of them what the true one
         // does, and 0 and -inf as they are)
@@ -184,9 +184,13 @@ template <typename OutT> struct GradEpilogue {
     int32_t classes;
 
     template <int N>
-    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, uint32_t (&r)[N],
-                                           uint8_t *patch) const
+    __device__ __forceinline__ void finish(const tc::Shape &s, const tc::Tile &tl, int row0, int lane, int c0, int end, bool ok,
+                                           uint32_t (&r)[N], uint8_t *patch) const
     {
+        if (!ok) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) r[j] = 0x7fffffffu;
+        }
         const bool whole = partial || keep;
         const TwoScales f = whole ? TwoScales(1.f, 1.f) : scales_of(scale, scale_b);
         const uint32_t zeros = __ballot_sync(0xffffffffu, labels && row0 + lane < s.m && (uint32_t)labels[row0 + lane] >= (uint32_t)classes);

@@ -19,8 +19,9 @@
 // each with an accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a
 // chunk the small products of planes come first.
 //
-// Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's copies and products in flight are
-// waited for (within the same limit, all of them together) and tensor memory is given back before it returns.
+// Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's tiles that are not finished come out NaN, its
+// copies and products in flight are waited for (within the same limit, all of them together) and tensor memory is given back
+// before it returns.
 #pragma once
 
 #include <cuda.h>
@@ -226,9 +227,10 @@ template <int CG, int BN> struct Layout {
 // whole rows are free of bank conflicts. Results go through it so that a warp's store covers 8 rows of 64 bytes, not 32 of 16.
 __device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { return reinterpret_cast<uint4 *>(patch + r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); }
 
-// Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end,
+// Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end, bool ok,
 // uint32_t (&acc)[N], uint8_t *patch) const`: called by the epilogue warps, lane by lane with N columns col .. of row
-// row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). All lanes
+// row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). Not ok: the
+// CTA has stopped, acc holds nothing, and the tile's results are to be NaN. All lanes
 // call. kChunked: every chunk has an accumulator, and finish gets the sums of all columns of the warp; else a tile has one, and
 // finish gets Epi::kStep columns at a time (0: all).
 template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
@@ -377,7 +379,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         uint8_t *patch = smem_raw + (ring - smem_u32(smem_raw)) + L::kStages * L::kStageBytes + (warp - 2) * kPatchBytes;
         uint32_t n_chunk = 0;
         bool ok = true;
-        for (int64_t t = first_tile; ok && t < tiles; t += stride) {
+        for (int64_t t = first_tile; t < tiles; t += stride) { // (stopped: the tiles that are left come out NaN)
             const Tile tl = tile_of(s, t);
             const int row0 = (tl.m * CG + (int)rank) * L::kBM + quarter * 32, col = tl.n * s.cols + part * kN;
             const int end = min(s.n, (tl.n + 1) * s.cols); // the tile's columns end here
@@ -385,25 +387,25 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             if constexpr (!kChunked) {
                 constexpr int kStep = Epi::kStep ? Epi::kStep : kN;
                 const uint32_t a = n_chunk & 1;
-                ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, s.limit, &s_answer[a], threadIdx.x == 64);
-                if (!ok) break;
+                if (ok) ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, s.limit, &s_answer[a], threadIdx.x == 64);
                 ++n_chunk;
                 fence_after();
 #pragma unroll 1
                 for (int c = 0; c < kN && col + c < end; c += kStep) {
                     uint32_t r[kStep];
+                    // (stopped: loaded all the same, a branch around the loads costs the full-width epilogues 800 bytes of spills)
 #pragma unroll
                     for (int j = 0; j < kStep; j += 32)
                         if (j == 0 || col + c + j < end) load32(at + a * BN + c + j, *reinterpret_cast<uint32_t(*)[32]>(&r[j]));
                     wait_loads();
-                    epi.template finish<kStep>(s, tl, row0, lane, col + c, end, r, patch);
+                    epi.template finish<kStep>(s, tl, row0, lane, col + c, end, ok, r, patch);
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[a]), 0) : smem_u32(&s_free[a]));
+                if (ok && lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[a]), 0) : smem_u32(&s_free[a]));
             } else {
             uint32_t acc[kN];
-            for (int c0 = tl.first; c0 < tl.last; c0 += s.chunk, ++n_chunk) {
+            for (int c0 = tl.first; ok && c0 < tl.last; c0 += s.chunk, ++n_chunk) {
                 const uint32_t a = n_chunk & 1;
                 ok = epilogue_wait(smem_u32(&s_done[a]), (n_chunk >> 1) & 1, &s_stop, s.limit, &s_answer[a], threadIdx.x == 64);
                 if (!ok) break;
@@ -428,7 +430,7 @@ k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 __syncwarp();
                 if (lane == 0) bar_arrive_cluster(CG == 2 ? map_rank(smem_u32(&s_free[a]), 0) : smem_u32(&s_free[a]));
             }
-            if (ok) epi.template finish<kN>(s, tl, row0, lane, col, end, acc, patch);
+            epi.template finish<kN>(s, tl, row0, lane, col, end, ok, acc, patch);
             }
             __syncwarp();
         }

@@ -65,3 +65,28 @@ for n, v, d in %r:
         out, status, labels, seconds = run(n, v, d, torch.bfloat16, grad)
         assert status == 0 and all(torch.isfinite(t).all() for t in out)
 """ % (SIZES,), None)
+
+
+@pytest.mark.parametrize("tile", [0, 1, 5])
+def test_what_was_not_computed_is_nan(tile):
+    """Without a status word, too: a result is NaN or within its bound, rows without a label are 0, and where no tile has its
+    operands everything else is NaN."""
+    in_a_process("""
+from operator_util import softmax_reference
+for n, v, d in %r + [(500, 3000, 600)]:
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        x, w, labels, weights = inputs(n, v, d, dtype, without=0.2 if n > 1 else 0.0)
+        want = softmax_reference(x, w, labels, weights, 0.5)
+        has = labels >= 0
+        for f in (lambda: ops.softmax_loss(x, w, labels), lambda: ops.softmax_loss_grad(x, w, labels, weights=weights, scale=0.5)):
+            out = dict(zip(("loss", "lse", "dx", "dw"), f()))
+            for name, t in out.items():
+                ref, off = want[name]
+                wrong = torch.isnan(t)
+                assert (wrong | ((t.double() - ref).abs() <= off)).all(), (name, n, v, d, dtype)
+                if name != "dw":
+                    assert not t[~has].any(), (name, n, v, d, dtype)
+                if %d == 0:
+                    assert (wrong if name == "dw" else wrong[has]).all(), (name, n, v, d, dtype)
+            assert torch.isnan(out["loss"]).any() or %d > 1, (n, v, d, dtype)
+""" % (SIZES, tile, tile), tile)
