@@ -14,10 +14,11 @@
 // in fp32 is off by, too), and of elements below 2^-17 of the largest by 2^-39 of that. Three products of planes (1+0, 0+1,
 // 0+0) are summed into one accumulator; the fourth is below 2^-22 of a term. `pairs` is 1, 3, or 2: A alone in two planes.
 //
-// The tensor cores cut an accumulator off towards zero at every step of 16, about 2^-25 of it on average (measured: sums of
-// 12 000 steps came out 1.3e-5 too small). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices,
-// each with an accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a
-// chunk the small products of planes come first.
+// The tensor cores cut an accumulator's low bits off at every step of 16 terms, and the terms' below them: up to 1.6e-7 of the
+// accumulator per step, always with the same sign (measured: sums of 131072 terms of one sign came out 5e-4 too small, of both signs
+// with 12 000 steps 1.3e-5). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices, each with an
+// accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a chunk the small products
+// of planes come first. Long sums for 16-bit results are cut into splits.
 //
 // Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's tiles that are not finished come out NaN, its
 // copies and products in flight are waited for (within the same limit, all of them together) and tensor memory is given back

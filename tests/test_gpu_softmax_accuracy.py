@@ -94,3 +94,51 @@ def test_both_signs_in_16_bits(ops, n, v, d, dtype):
     roundings = 1.0 if n <= 32 else 2.0 ** 0.5
     for s, t in ((gx, dx), (gw, dw)):
         assert off(s, t, t.norm()) <= 1.1 * roundings * HALF[dtype] / 3 ** 0.5
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=NAMES.get)
+def test_very_many_classes_of_one_sign(ops, dtype):
+    """What accumulators cut off has one sign, so it shows in the mean error: an eighth of half a step of the sums' magnitudes at
+    most. Beside it the roundings' mean: of P's entry of the label, one per row (half / sqrt(3) of half of the magnitudes, the mean of
+    32 rows, three times that), of the results (of 32 x 1024 of them: nothing)."""
+    n, v, d, step = 2048, 3_000_000, 1024, 100_000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = (torch.randn(n, d, generator=g, device="cuda") / d ** 0.5).to(dtype)
+    w = torch.empty(v, d, dtype=dtype, device="cuda")
+    for a in range(0, v, step):
+        w[a:a + step] = (torch.randn(step, d, generator=g, device="cuda") + 3.0).to(dtype)
+    labels = torch.randint(0, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+    weights = torch.rand(n, generator=g, device="cuda") + 0.5
+    dx = ops.softmax_loss_grad(x, w, labels, weights=weights)[2]
+    rows = torch.arange(0, n, n // 32, device="cuda")
+    X = x[rows].double()
+    p = torch.softmax(torch.cat([X @ w[a:a + step].double().T for a in range(0, v, step)], 1), 1)
+    p[torch.arange(len(rows)), labels[rows].long()] -= 1.0
+    p *= weights[rows].double()[:, None]
+    want, size = torch.zeros_like(X), torch.zeros_like(X)
+    for a in range(0, v, step):
+        b = w[a:a + step].double()
+        want += p[:, a:a + step] @ b
+        size += p[:, a:a + step].abs() @ b.abs()
+    mean = float(((dx[rows].double() - want) / size).mean())
+    assert abs(mean) <= HALF[dtype] * (1 / 8 + 3 * 0.5 / 3 ** 0.5 / 32 ** 0.5), mean
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=NAMES.get)
+def test_very_many_rows_of_one_sign(ops, dtype):
+    """The same of dW: an eighth, and the results' roundings (of 16 x 64 of them, three times their mean)."""
+    n, v, d = 4_000_000, 16, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = (torch.randn(n, d, generator=g, device="cuda") / 8 + 3.0).to(dtype)
+    w = (torch.randn(v, d, generator=g, device="cuda") / 8).to(dtype)
+    labels = torch.randint(0, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+    weights = torch.rand(n, generator=g, device="cuda") + 0.5
+    scale = 2.0 ** -14
+    dw = ops.softmax_loss_grad(x, w, labels, weights=weights, scale=scale)[3]
+    want, size = torch.zeros(v, d, dtype=torch.float64, device="cuda"), torch.zeros(v, d, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 500_000):
+        _, p, _, part = exact(x[a:a + 500_000], w, labels[a:a + 500_000], scale, weights[a:a + 500_000])
+        want += part
+        size += p.abs().T @ x[a:a + 500_000].double().abs()
+    mean = float(((dw.double() - want) / size).mean())
+    assert abs(mean) <= HALF[dtype] * (1 / 8 + 3 / 3 ** 0.5 / 1024 ** 0.5), mean

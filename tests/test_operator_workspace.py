@@ -38,3 +38,9 @@ def test_sizes_with_room_are_as_they_were(b):
     for type, planes in ((0, 2), (1, 1), (2, 1)):
         a, c = size_of(b, 1 << 14, 131072, 64, type), size_of(b, 1 << 16, 131072, 64, type)
         assert c - a == planes * ((1 << 16) - (1 << 14)) * 64 * 2
+
+
+@pytest.mark.parametrize("type", [0, 1, 2])
+@pytest.mark.parametrize("grad", [0, 1])
+def test_no_rows(b, type, grad):
+    assert size_of(b, 0, 100, 8, type, grad) >= 0
