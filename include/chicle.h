@@ -320,10 +320,12 @@ typedef struct {
 /* Softmax cross entropy of the linear map X W^T to W->rows classes: with l_iv = x_i . w_v,
  *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, label_i},
  * one float per row each. A row whose label is negative has no label: its loss and lse are 0, and what it holds has no
- * effect. X and W have one type; products are summed in fp32, and the logits are not kept. fp32 elements are
- * taken to 2^-22 of themselves, or 2^-39 of the largest magnitude in their matrix where that is more (rows without a label left
- * out): as exact as a sum in fp32, unless magnitudes within a matrix are further apart than 2^17. Values that are not finite give results that are not finite. chicle_softmax_workspace gives the bytes of workspace
- * (256-byte aligned) for the same descriptions (host only, no device is touched). */
+ * effect. X and W have one type; products are summed in fp32, and the logits are not kept. fp32 elements are taken to
+ * 2^-22 of themselves, or 2^-39 of the largest magnitude in their matrix where that is more (rows without a label left
+ * out): as exact as a sum in fp32 (sums of one sign: 3e-6 of it), unless magnitudes within a matrix are further apart than
+ * 2^17. Values that are not finite give results that are not finite; but for 16-bit types a logit of -inf is a class of
+ * probability 0. chicle_softmax_workspace gives the bytes of workspace (256-byte aligned) for the same descriptions (host
+ * only, no device is touched). */
 chicle_status_t chicle_softmax_workspace(const chicle_dense_t *X, const chicle_dense_t *W, int gradients, size_t *host_bytes);
 chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
                                     const int32_t *dev_labels, float *dev_loss, float *dev_lse, void *dev_workspace,
@@ -332,9 +334,11 @@ chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_
 /* The same, and the gradients of  scale * sum_i weight_i loss_i  (dev_weights: one float per row, or NULL for 1; scale
  * finite) with respect to X and W, in their types: every element of dX and dW is written (rows of dX without a label are
  * 0; their weights have no effect either). The rows' weighted differences of probability and label are held to 2^-39 of the
- * largest weight of a row with a label in fp16 and fp32: rows whose weights are further below it lose bits of their gradients. dX and dW overlap neither X, W nor each other. The logits are held for about two gigabytes of rows at a time (8 GiB at
- * most, if that holds a row; beside them a 32nd of that for sums), and where there are several such pieces, dW is summed in fp32
- * in the workspace. */
+ * largest weight of a row with a label in fp16 and fp32: rows whose weights are further below it lose bits of their
+ * gradients. With more than 32 rows of 16-bit type these differences are rounded to that type, once, as the gradients are: the
+ * two roundings together are 1.41 times that of the gradients alone. dX and dW overlap neither X, W nor each other. The
+ * logits are held for about two gigabytes of rows at a time (8 GiB at most, if that holds a row; beside them a 32nd of that
+ * for sums), and where there are several such pieces, dW is summed in fp32 in the workspace. */
 chicle_status_t chicle_softmax_loss_grad(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
                                          const int32_t *dev_labels, const float *dev_weights, float scale, float *dev_loss,
                                          float *dev_lse, const chicle_dense_t *dX, const chicle_dense_t *dW, void *dev_workspace,
@@ -365,8 +369,8 @@ typedef struct {
 
 /* *dev_norm = the 2-norm of all elements of all tensors (squares summed in fp64 in a fixed order), and
  * out = in * min(1, max_norm / (norm + 1e-6)) for each of them. A *dev_norm that is not finite (beyond fp32, too) leaves the
- * elements as they are (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors is a host array, read
- * during the call. An out is the tensor's own in or overlaps neither any in nor another out (a tensor listed twice with a result
+ * elements as they are (out = in), so that the caller can look at the norm and skip the step. max_norm >= 0. host_tensors
+ * is a host array, read during the call. An out is the tensor's own in or overlaps neither any in nor another out (a tensor listed twice with a result
  * is refused; without results it counts twice). Workspace: CHICLE_CLIP_WORKSPACE bytes, 256-byte aligned. */
 #define CHICLE_CLIP_WORKSPACE 16384
 chicle_status_t chicle_clip_gradients(int device, void *cuda_stream, int64_t count, const chicle_tensor_t *host_tensors, float max_norm,

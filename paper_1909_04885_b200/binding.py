@@ -454,7 +454,8 @@ def chunks_rebalance_step(task, chunk_off, K: int, time_per_sample):
 # calls, no call synchronises, all can be captured into a CUDA graph. No autograd graph is recorded. `status`: an optional
 # int32 CUDA tensor of one element whose bits the kernels set (STATUS_BAD_ID: a label or id beyond the last class or row,
 # taken as none; STATUS_TIMEOUT: the results are not valid, and what is concerned of them is NaN with or without a status). What is
-# written in place (out, the clipped tensors) is written behind autograd's back: version counters stay as they are.
+# written in place (out, the clipped tensors) is written behind autograd's back: version counters stay as they are. With `stream`, the
+# inputs are the caller's to keep until the work is done: they are not recorded for that stream with the allocator.
 STATUS_BAD_ID, STATUS_TIMEOUT = 4, 8
 CLIP_WORKSPACE = 16384
 _ERR_LEN = 256

@@ -781,6 +781,9 @@ int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs, int64_t longest)
 // of the result: 768 steps in fp16, 6144 in bf16. (One accumulator for 131072 classes: 2.5e-4 off, half of fp16's half step; for
 // 800000: 1.7e-3. The planes cost 1024 x 200000 x 1024 in fp16 1.60 ms instead of 1.48, 8192 x 131072 x 4096 in bf16 nothing that shows.)
 constexpr int64_t kLongestF16 = 768 * 16 / tc::kBK, kLongestBf16 = 6144 * 16 / tc::kBK;
+// Logits of a piece. Nothing hangs on where a piece ends: 8192 rows of 131072 classes and 4096 columns in bf16 take 23.7 ms in one
+// piece, 8193 in two 23.7 to 24.0; with 2^30 instead 23.0 and 24.2, 16384 rows 46.3 and 48.0 with 2^31, of 1024 columns 13.4 and 13.1
+// (one GPU's power limit moves these by 4 %).
 constexpr int64_t kPieceBytes = (int64_t)1 << 31;
 constexpr int64_t kFewRows = 32;
 constexpr int64_t kStatBytes = (int64_t)1 << 30; // the loss alone: pairs of (largest, sum), for so many bytes of rows at a time

@@ -231,9 +231,10 @@ __device__ __forceinline__ uint4 *patch_at(uint8_t *patch, int r, int c) { retur
 // Epi has `template <int N> __device__ void finish(const Shape &, const Tile &, int row0, int lane, int col, int end, bool ok,
 // uint32_t (&acc)[N], uint8_t *patch) const`: called by the epilogue warps, lane by lane with N columns col .. of row
 // row0 + lane of C (rows behind the last and columns from `end` on are not C's: what acc holds there is undefined). Not ok: the
-// CTA has stopped, acc holds nothing, and the tile's results are to be NaN. All lanes
-// call. kChunked: every chunk has an accumulator, and finish gets the sums of all columns of the warp; else a tile has one, and
-// finish gets Epi::kStep columns at a time (0: all).
+// CTA has stopped, acc holds nothing, and the tile's results are to be NaN. All lanes call. kChunked: every chunk has an
+// accumulator, and finish gets the sums of all columns of the warp (128 sums, and 32 more on their way: 168 registers, the most
+// that 320 threads can have, and about 100 bytes of spills with tiles of 256); else a tile has one, and finish gets Epi::kStep
+// columns at a time (0: all).
 template <int CG, int BN, bool AMN, bool BMN, bool kChunked, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s, const Epi epi)

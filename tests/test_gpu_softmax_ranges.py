@@ -66,3 +66,27 @@ def test_single_precision_of_large_operands_with_logits_of_zero(ops, n, v):
     for got, a, b, k in ((dx, p, w.double(), v), (dw, p.T, x.double(), n)):
         off = (3 * k + 32) * 2.0 ** -23 * (a.abs() @ b.abs()) + 2.0 ** -38 * a.abs().sum(1, keepdim=True) * b.abs().max()
         assert ((got.double() - a @ b).abs() <= off).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=NAMES.get)
+@pytest.mark.parametrize("n,v,d", [(40, 300, 64), (300, 700, 1100)])
+def test_classes_with_a_logit_of_minus_infinity(ops, n, v, d, dtype):
+    """Rows of x above zero, two classes of -inf (one of them all that its block holds but for another): their probability is 0; a row
+    with such a label has an infinite loss."""
+    x, w, labels, weights = inputs(n, v, d, dtype)
+    x = x.abs() + 0.125
+    w[:, 1:] *= 0.25
+    gone = [5, v - 1]
+    stay = [k for k in range(v) if k not in gone]
+    labels = torch.where((labels == 5) | (labels == v - 1), torch.full_like(labels, 6), labels)
+    w[gone] = -float("inf")
+    at = torch.tensor([stay.index(int(k)) for k in labels.tolist()], dtype=torch.int32, device="cuda")
+    want = softmax_reference(x, w[stay], at, weights)
+    for out in (ops.softmax_loss(x, w, labels), ops.softmax_loss_grad(x, w, labels, weights=weights)):
+        check(out[0], want["loss"], "loss")
+        check(out[1], want["lse"], "lse")
+    check(out[3][stay], want["dw"], "dw")
+    assert not out[3][gone].any()
+    labels[3] = 5
+    for out in (ops.softmax_loss(x, w, labels), ops.softmax_loss_grad(x, w, labels)):
+        assert out[0][3] == float("inf") and torch.isfinite(out[0][:3]).all() and torch.isfinite(out[1]).all()
