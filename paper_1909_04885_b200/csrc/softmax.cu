@@ -756,19 +756,18 @@ bool takes_bulk(const chicle_dense_t &x)
 }
 
 // The summed index of a gradient is cut where its tiles alone would leave SMs idle: time of the waves plus that of
-// writing and joining the planes. `longest`: slices that an accumulator may take (0: any number); longer sums are cut, too.
-int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs, int64_t longest)
+// writing and joining the planes.
+int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs)
 {
-    const int least = longest ? (int)std::max<int64_t>(1, ceil_div(steps * pairs, longest)) : 1;
     const int rows = tile_rows(m), cols = tile_columns(n);
     const int64_t tiles = ceil_div(m, rows) * ceil_div(n, cols), slots = kSms / (rows / 128);
     const double slice = cols == 256 ? 0.28e-6 : 0.25e-6; // (narrow tiles wait for their copies: three quarters of the bytes)
-    int best = least;
+    int best = 1;
     double best_t = 0;
-    for (int s = least; s <= std::max(64, least) && s <= steps; ++s) {
+    for (int s = 1; s <= 64 && s <= steps; ++s) {
         const double waves = (double)ceil_div(tiles * s, slots);
         const double t = waves * ((double)(ceil_div(steps, s) * pairs) * slice + 1.0e-6) + (s > 1 ? 6e-6 + (double)s * m * n * 8.0 / 5e12 : 0.0);
-        if (s == least || t < best_t * 0.95) {
+        if (s == 1 || t < best_t * 0.95) {
             best = s;
             best_t = t;
         }
@@ -779,7 +778,7 @@ int plan_splits(int64_t m, int64_t n, int64_t steps, int pairs, int64_t longest)
 // Slices that an accumulator of a 16-bit gradient takes. What it cuts off, 1.6e-7 of itself per step of 16 terms where the terms have
 // one sign (tensor_core.cuh), comes to half of that times the steps, of the terms' magnitudes, and stays below an eighth of half a step
 // of the result: 768 steps in fp16, 6144 in bf16. (One accumulator for 131072 classes: 2.5e-4 off, half of fp16's half step; for
-// 800000: 1.7e-3. The planes cost 1024 x 200000 x 1024 in fp16 1.60 ms instead of 1.48, 8192 x 131072 x 4096 in bf16 nothing that shows.)
+// 800000: 1.7e-3.) Longer sums are added chunk by chunk in registers.
 constexpr int64_t kLongestF16 = 768 * 16 / tc::kBK, kLongestBf16 = 6144 * 16 / tc::kBK;
 // Logits of a piece. Nothing hangs on where a piece ends: 8192 rows of 131072 classes and 4096 columns in bf16 take 23.7 ms in one
 // piece, 8193 in two 23.7 to 24.0; with 2^30 instead 23.0 and 24.2, 16384 rows 46.3 and 48.0 with 2^31, of 1024 columns 13.4 and 13.1
@@ -797,6 +796,7 @@ struct Plan {
     int64_t pitch_d, ld_v;
     int64_t piece;     // rows per piece
     int logit_chunk, grad_chunk; // slices per accumulator
+    int longest;                 // and of a gradient of 16 bits, where its sum has more
     int cols, parts;   // of the logits' tiles
     int splits_x, splits_w;
     // offsets into the workspace
@@ -822,9 +822,10 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     p.ld_v = (p.v + 63) / 64 * 64;
     // Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential
     // takes on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 512:
-    // 7e-7, 256: 4e-7). A gradient that is rounded to 16 bits in the end has one accumulator for kLongest of them.
+    // 7e-7, 256: 4e-7). A gradient that is rounded to 16 bits in the end has one accumulator for `longest` of them.
     p.logit_chunk = (p.wide ? 512 : 1024) / tc::kBK;
     p.grad_chunk = (p.wide ? 512 : 1024) / tc::kBK; // (16 bits, P in two planes: what is fetched again is still in L2)
+    p.longest = (int)((p.half ? kLongestF16 : kLongestBf16) / p.grad_pairs);
     p.parts = tc::kEpiWarps / 4;
     p.cols = logit_columns(p.n, p.v, p.parts, grad);
     size_t at = 0;
@@ -864,9 +865,8 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
             p.store = p.p = take((size_t)p.piece * p.ld_v * 2);
         }
         if (p.piece < p.n) p.acc = take((size_t)p.v * p.d * 4);
-        const int64_t longest = p.wide ? 0 : p.half ? kLongestF16 : kLongestBf16;
-        p.splits_x = plan_splits(p.piece, p.d, ceil_div(p.v, tc::kBK), p.grad_pairs, longest);
-        p.splits_w = plan_splits(p.v, p.d, ceil_div(p.piece, tc::kBK), p.grad_pairs, longest);
+        p.splits_x = plan_splits(p.piece, p.d, ceil_div(p.v, tc::kBK), p.grad_pairs);
+        p.splits_w = plan_splits(p.v, p.d, ceil_div(p.piece, tc::kBK), p.grad_pairs);
         size_t part = 0;
         if (p.splits_x > 1) part = (size_t)p.splits_x * p.piece * p.d * 4;
         if (p.splits_w > 1) part = std::max(part, (size_t)p.splits_w * p.v * p.d * 4);
@@ -951,7 +951,18 @@ int group_of(int64_t k, int planes, int rows_per_tile)
 template <typename OutT>
 cudaError_t gradient(const Plan &p, const Operand &a, const Operand &b, bool of_x, tc::Shape s, GradEpilogue<OutT> epi, cudaStream_t stream)
 {
-    cudaError_t e = of_x ? run_product<false, true, sizeof(OutT) == 4>(a, b, s, tile_columns(s.n), epi, stream) : run_product<true, true, sizeof(OutT) == 4>(a, b, s, tile_columns(s.n), epi, stream);
+    const int cols = tile_columns(s.n);
+    bool chunked = true;
+    if constexpr (sizeof(OutT) == 2) {
+        chunked = ceil_div(s.k_steps, s.splits) > p.longest;
+        if (chunked) s.chunk = p.longest;
+    }
+    cudaError_t e;
+    if (chunked) {
+        e = of_x ? run_product<false, true, true>(a, b, s, cols, epi, stream) : run_product<true, true, true>(a, b, s, cols, epi, stream);
+    } else if constexpr (sizeof(OutT) == 2) {
+        e = of_x ? run_product<false, true, false>(a, b, s, cols, epi, stream) : run_product<true, true, false>(a, b, s, cols, epi, stream);
+    }
     if (e == cudaSuccess && s.splits > 1) {
         const int64_t all = (int64_t)s.m * s.n;
         auto *join = (s.n & 3) == 0 ? k_join_splits<OutT, 4> : k_join_splits<OutT, 1>;

@@ -18,7 +18,7 @@
 // accumulator per step, always with the same sign (measured: sums of 131072 terms of one sign came out 5e-4 too small, of both signs
 // with 12 000 steps 1.3e-5). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices, each with an
 // accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a chunk the small products
-// of planes come first. Long sums for 16-bit results are cut into splits.
+// of planes come first.
 //
 // Every wait is bounded in time; a wait that runs out sets a status bit, the CTA's tiles that are not finished come out NaN, its
 // copies and products in flight are waited for (within the same limit, all of them together) and tensor memory is given back
