@@ -320,12 +320,12 @@ typedef struct {
 /* Softmax cross entropy of the linear map X W^T to W->rows classes: with l_iv = x_i . w_v,
  *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, label_i},
  * one float per row each. A row whose label is negative has no label: its loss and lse are 0, and what it holds has no
- * effect. X and W have one type; products are summed in fp32, and the logits are not kept. fp32 elements are taken to
- * 2^-22 of themselves, or 2^-39 of the largest magnitude in their matrix where that is more (rows without a label left
- * out): as exact as a sum in fp32 (sums of one sign: 3e-6 of it), unless magnitudes within a matrix are further apart than
- * 2^17. Values that are not finite give results that are not finite; but for 16-bit types a logit of -inf is a class of
- * probability 0. chicle_softmax_workspace gives the bytes of workspace (256-byte aligned) for the same descriptions (host
- * only, no device is touched). */
+ * effect. X and W have one type; products are summed in fp32 by the tensor cores (a logit whose terms have one sign is off by
+ * up to 6e-6 of itself), and the logits are not kept. fp32 elements are taken to 2^-22 of themselves, or 2^-39 of the largest
+ * magnitude in their matrix where that is more (rows without a label left out): about as exact as a sum in fp32, unless
+ * magnitudes within a matrix are further apart than 2^17. Values that are not finite give results that are not finite; but
+ * for 16-bit types a logit of -inf is a class of probability 0. chicle_softmax_workspace gives the bytes of workspace
+ * (256-byte aligned) for the same descriptions (host only, no device is touched). */
 chicle_status_t chicle_softmax_workspace(const chicle_dense_t *X, const chicle_dense_t *W, int gradients, size_t *host_bytes);
 chicle_status_t chicle_softmax_loss(int device, void *cuda_stream, const chicle_dense_t *X, const chicle_dense_t *W,
                                     const int32_t *dev_labels, float *dev_loss, float *dev_lse, void *dev_workspace,

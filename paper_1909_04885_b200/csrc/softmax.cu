@@ -820,10 +820,11 @@ Plan make_plan(const chicle_dense_t &X, const chicle_dense_t &W, bool grad)
     // rows of whole 128-byte lines: a row of a bulk copy that straddles two takes two requests
     p.pitch_d = (p.d + 63) / 64 * 64;
     p.ld_v = (p.v + 63) / 64 * 64;
-    // Slices per accumulator (why: tensor_core.cuh): 1024 elements of a logit from 16-bit operands, whose errors its exponential
-    // takes on whole (4096: loss off by 1.2e-6, 1024: 3e-7); 512 of single precision (gradients with 2048: off by 2.5e-6, 512:
-    // 7e-7, 256: 4e-7). A gradient that is rounded to 16 bits in the end has one accumulator for `longest` of them.
-    p.logit_chunk = (p.wide ? 512 : 1024) / tc::kBK;
+    // Slices per accumulator (why: tensor_core.cuh): 512 elements of a logit, whose errors its exponential takes on whole (16 bits, terms
+    // of one sign: 1024 are off by 6e-6 of the logit, 512 by 3e-6; of both signs loss off by 3e-7 and 1.5e-7; 4096 x 100000 x 2048 takes
+    // 1355 us with 1024, 1403 with 512, 1527 with 256), and of a gradient in single precision (2048: off by 2.5e-6, 512: 7e-7, 256:
+    // 4e-7). A gradient that is rounded to 16 bits in the end has one accumulator for `longest` of them.
+    p.logit_chunk = 512 / tc::kBK;
     p.grad_chunk = (p.wide ? 512 : 1024) / tc::kBK; // (16 bits, P in two planes: what is fetched again is still in L2)
     p.longest = (int)((p.half ? kLongestF16 : kLongestBf16) / p.grad_pairs);
     p.parts = tc::kEpiWarps / 4;

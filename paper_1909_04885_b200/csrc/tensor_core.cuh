@@ -14,7 +14,7 @@
 // in fp32 is off by, too), and of elements below 2^-17 of the largest by 2^-39 of that. Three products of planes (1+0, 0+1,
 // 0+0) are summed into one accumulator; the fourth is below 2^-22 of a term. `pairs` is 1, 3, or 2: A alone in two planes.
 //
-// The tensor cores cut an accumulator's low bits off at every step of 16 terms, and the terms' below them: up to 1.6e-7 of the
+// The tensor cores cut an accumulator's low bits off at every step of 16 terms, and the terms' below them: 1.6e-7 to 1.9e-7 of the
 // accumulator per step, always with the same sign (measured: sums of 131072 terms of one sign came out 5e-4 too small, of both signs
 // with 12 000 steps 1.3e-5). So a sum that has to keep fp32's accuracy is cut into chunks of `chunk` slices, each with an
 // accumulator of its own in tensor memory, and the epilogue's warps add the chunks in registers; inside a chunk the small products

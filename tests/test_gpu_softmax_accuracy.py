@@ -142,3 +142,21 @@ def test_very_many_rows_of_one_sign(ops, dtype):
         size += p.abs().T @ x[a:a + 500_000].double().abs()
     mean = float(((dw.double() - want) / size).mean())
     assert abs(mean) <= HALF[dtype] * (1 / 8 + 3 / 3 ** 0.5 / 1024 ** 0.5), mean
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("n,v,d", [(1, 3000, 4096), (300, 700, 4096), (300, 700, 1000)])
+def test_logits_of_one_sign(ops, n, v, d, dtype):
+    """An accumulator of a logit takes 64 steps (single precision: 32 that count, the small products of planes come first); a step cuts
+    off 1.6e-7 of it, of a growing sum half of that: 64 x 1.6e-7 / 2 = 5.1e-6 of the logit; chunks, planes, exponentials: 2^-20."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(n, d, generator=g, device="cuda").abs().to(dtype)
+    w = (torch.randn(v, d, generator=g, device="cuda").abs() / 8).to(dtype)
+    labels = torch.randint(0, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+    logits = x.double() @ w.double().T
+    want = torch.logsumexp(logits, 1)
+    own = logits.gather(1, labels.long()[:, None])[:, 0]
+    bound = 5.1e-6 + 2.0 ** -20
+    for out in (ops.softmax_loss(x, w, labels), ops.softmax_loss_grad(x, w, labels)):
+        assert ((out[1].double() - want).abs() <= bound * want).all()
+        assert ((out[0].double() - (want - own)).abs() <= bound * want).all()

@@ -1,5 +1,5 @@
-"""Softmax cross entropy where a logit is the sum of several chunks, each with an accumulator of its own (more than 1024 columns
-of 16 bits, more than 512 of single precision), on the GPU. Bounds: operator_util."""
+"""Softmax cross entropy where a logit is the sum of several chunks, each with an accumulator of its own (more than 512
+columns), on the GPU. Bounds: operator_util."""
 import pytest
 
 pytestmark = pytest.mark.gpu
